@@ -29,6 +29,8 @@
  *                          layout tree_verify_attention streams fastest
  *   tree_commit            appends the accepted path's K/V rows to the cache and
  *                          advances the prefix lengths (closes the step's loop)
+ *   prompt_attention       causal attention of whole prompts (the prefill whose
+ *                          K/V rows become the cached prefix)
  *
  * Conventions
  *   - Every function returns int32_t: SMART_OK (0) or a negative error code.
@@ -80,6 +82,18 @@ enum { SMART_TVA_BAD_BLOCK = 1 };
 /* Element type of an fp8 KV cache (cache only; q, tree k / v and outputs stay SMART_F32 / SMART_BF16):
  * E4M3 of the OCP 8-bit floating point specification (bias 7, no infinities, largest value 448). */
 enum { SMART_FP8_E4M3 = 2 };
+/* Element type of a 4-bit KV cache (cache only): E2M1 of the OCP microscaling formats (0, 0.5, 1, 1.5, 2, 3, 4, 6 and their
+ * negatives; code bit 3 is the sign), where the 32 consecutive head dims 32 j .. 32 j + 31 of one token share the scale
+ * 2^(s - 127) of a byte s (255: all of them are NaN).  The caches count in bytes, strides included, and have a page layout
+ * of their own (kv_layout must be SMART_KV_INTERLEAVED, of which it is the 4-bit form).  A page holds
+ * SMART_FP4_PAGE_BYTES(block_size, head_dim) bytes, a byte two codes, the even head dim's in its low half:
+ *   K: element (slot, d) in byte ((d / 32) * block_size + slot) * 16 + (d % 32) / 2, its scale in byte
+ *      block_size * head_dim / 2 + slot * (head_dim / 32) + d / 32
+ *   V: element (slot, d) in byte ((slot / 8) * (head_dim / 4) + d / 4) * 16 + (slot % 8) * 2 + (d % 4) / 2, its scale in byte
+ *      block_size * head_dim / 2 + (d / 32) * block_size + slot
+ * block_size must be a multiple of 8, head_dim of 32; cache pointers and strides multiples of 16 bytes. */
+enum { SMART_FP4_E2M1 = 3 };
+#define SMART_FP4_PAGE_BYTES(block_size, head_dim) ((int64_t)(block_size) * (head_dim) / 2 + (int64_t)(block_size) * (head_dim) / 32)
 
 /* Paged KV-cache layouts.  A page is the block_size x head_dim elements of one
  * (physical block, kv head); pages are addressed by block_stride / head_stride
@@ -533,6 +547,36 @@ int32_t kv_cache_write_fp8(smart_ctx* ctx, void* stream, int32_t src_dtype, int3
                            int64_t cache_token_stride /* PLAIN only */, float k_scale, float v_scale);
 
 /* ---------------------------------------------------------------------------
+ * kv_cache_write_fp4, kv_cache_read_fp4 (device)
+ *
+ * kv_cache_write into a 4-bit cache (SMART_FP4_E2M1), and rows of it back as
+ * values, for a program that hands a sequence to another cache.
+ * Writing: of 32 head dims that share a scale, with 2^e <= max |x| < 2^(e + 1),
+ * the scale is 2^(e - 2), or 2^(e - 1) where max |x| > 1.75 * 2^e, kept within
+ * 2^-125 .. 2^125 (zeros: 2^-125); every element becomes the E2M1 value nearest
+ * to x / scale, ties to the even code, saturating at +-6 (infinities too); a
+ * NaN makes all 32 NaN.  Head dims, kv heads and tokens do not share anything.
+ * Reading: row t of d_k_dst / d_v_dst ([n_tokens][num_kv_heads][head_dim], of
+ * dst_dtype; every value is exact in both types) is the row of slot
+ * d_slot_mapping[t]; rows of negative slots and of slots outside the cache
+ * become zero.
+ * A slot that one writing call names twice holds afterwards any mix of the rows.
+ * Errors: SMART_EINVAL (null pointers, sizes, dtype; caches, strides, sources
+ * and destinations that are not aligned to 16 bytes; strides smaller than a
+ * page).
+ * ------------------------------------------------------------------------- */
+int32_t kv_cache_write_fp4(smart_ctx* ctx, void* stream, int32_t src_dtype, int32_t n_tokens,
+                           int32_t num_kv_heads, int32_t head_dim, int32_t block_size, int32_t num_blocks,
+                           const void* d_k_src, const void* d_v_src, const int64_t* d_slot_mapping,
+                           void* d_k_cache, void* d_v_cache,
+                           int64_t cache_block_stride, int64_t cache_head_stride);
+int32_t kv_cache_read_fp4(smart_ctx* ctx, void* stream, int32_t dst_dtype, int32_t n_tokens,
+                          int32_t num_kv_heads, int32_t head_dim, int32_t block_size, int32_t num_blocks,
+                          const void* d_k_cache, const void* d_v_cache,
+                          int64_t cache_block_stride, int64_t cache_head_stride,
+                          const int64_t* d_slot_mapping, void* d_k_dst, void* d_v_dst);
+
+/* ---------------------------------------------------------------------------
  * tree_verify_attention (device)
  *
  * For every sequence b, node i of its tree, query head h (kv head g = h / G,
@@ -548,7 +592,9 @@ int32_t kv_cache_write_fp8(smart_ctx* ctx, void* stream, int32_t src_dtype, int3
  * block_size 16 / head_dim 128 rounds softmax weights to bf16 before the second
  * product, the others hold them in fp32).  With an fp8 cache (kv_cache_dtype =
  * SMART_FP8_E4M3) the cached keys and values are k_scale / v_scale times the
- * stored E4M3 values (exact in bf16); everything else is as above.  A tree's
+ * stored E4M3 values (exact in bf16); everything else is as above.  With a 4-bit
+ * cache (SMART_FP4_E2M1) they are the values that the page's codes and scales
+ * stand for (exact in bf16 as well).  A tree's
  * rows per kv head, n x G, are served in groups of up to 256 (of 128 by the
  * tiled kernel), each of which reads the prefix once.
  *
@@ -580,7 +626,8 @@ typedef struct {
   float softmax_scale;
   int32_t kv_cache_dtype; /* 0: the cache holds `dtype` elements; SMART_FP8_E4M3: one byte per element,
                              key = k_scale * stored value, value = v_scale * stored value (strides still
-                             count elements) */
+                             count elements); SMART_FP4_E2M1: 4-bit pages (strides count bytes, no token
+                             stride, no k_scale / v_scale) */
   const void* d_q;
   const void* d_k_tree;
   const void* d_v_tree;
@@ -744,6 +791,61 @@ int32_t tree_commit_fp8(smart_ctx* ctx, void* stream, int32_t src_dtype, int32_t
                         int64_t cache_block_stride, int64_t cache_head_stride,
                         int64_t cache_token_stride /* PLAIN only */,
                         int32_t* d_new_prefix_len, int32_t* d_status, float k_scale, float v_scale);
+
+/* tree_commit into a 4-bit cache (SMART_FP4_E2M1): rows are stored as kv_cache_write_fp4 does.  src_dtype is the type of
+ * d_k_tree / d_v_tree.  Everything else as tree_commit; errors also as for kv_cache_write_fp4. */
+int32_t tree_commit_fp4(smart_ctx* ctx, void* stream, int32_t src_dtype,
+                        int32_t batch, int32_t max_depth, int32_t num_kv_heads, int32_t head_dim,
+                        int32_t block_size, int32_t max_blocks_per_seq, int32_t num_blocks,
+                        const int32_t* d_cu_nodes, const int32_t* d_accept_len, const int32_t* d_accept_path,
+                        const void* d_k_tree, const void* d_v_tree,
+                        const int32_t* d_block_table, const int32_t* d_prefix_len,
+                        void* d_k_cache, void* d_v_cache, int64_t cache_block_stride,
+                        int64_t cache_head_stride, int32_t* d_new_prefix_len, int32_t* d_status);
+
+/* ---------------------------------------------------------------------------
+ * prompt_attention (device)
+ *
+ * Causal attention of whole prompts, packed one after the other: what the target
+ * model computes per layer before there is a prefix to verify trees against
+ * (its K and V rows are what kv_cache_write lays down; rotate with tree_rope
+ * first, whose positions may be any).  Prompt b holds tokens d_cu_tokens[b] ..
+ * d_cu_tokens[b + 1] - 1 and may be empty.  For token t of prompt b, query head h
+ * (kv head g = h / G, G = num_q_heads / num_kv_heads), over the tokens u <= t of
+ * the same prompt:
+ *   out[t,h,:] = softmax_u(softmax_scale * <q[t,h,:], k[u,g,:]>) . v[u,g,:]
+ *   lse[t,h]   = log sum_u exp(score)                        (optional)
+ * Scores, softmax and accumulation are fp32; with bf16 the softmax weights are
+ * rounded to bf16 before the second product and the sum that divides it is taken
+ * over the rounded ones (so that equal values come out as they are); lse is that
+ * of the unrounded weights.  What later tokens hold, infinities and NaN included,
+ * never enters a row.
+ * q, out [total_tokens][num_q_heads][head_dim], k, v [total_tokens][num_kv_heads]
+ * [head_dim]; the four token strides count elements, so q, k and v may be parts of
+ * one projection's output (heads and head dims are contiguous).  lse
+ * [total_tokens][num_q_heads].  Rows of no prompt (before d_cu_tokens[0], behind
+ * d_cu_tokens[batch]) are neither read nor written.  d_cu_tokens must be a running
+ * sum inside [0, total_tokens]; if it is not (checked on the device), no row is
+ * written.  Uses no workspace: it may be captured, and calls may overlap.
+ * Host errors: SMART_EINVAL for null pointers, Hq % Hkv != 0, head_dim not in
+ * {64, 128}, unknown dtype, softmax_scale not positive or not below 1e30,
+ * total_tokens x Hq >= 2^31, token strides smaller than a token's row, pointers or
+ * token strides that are not multiples of 16 bytes; SMART_EHIP.
+ * ------------------------------------------------------------------------- */
+typedef struct {
+  int32_t dtype; /* SMART_F32 | SMART_BF16: q, k, v, out share it */
+  int32_t batch, total_tokens, num_q_heads, num_kv_heads, head_dim;
+  float softmax_scale;
+  const void* d_q;
+  const void* d_k;
+  const void* d_v;
+  int64_t q_stride, k_stride, v_stride, out_stride; /* elements from one token to the next */
+  const int32_t* d_cu_tokens;                       /* [batch+1] */
+  void* d_out;
+  float* d_lse; /* [total_tokens][num_q_heads] or NULL */
+} prompt_params;
+
+int32_t prompt_attention(smart_ctx* ctx, void* stream, const prompt_params* params);
 
 #ifdef __cplusplus
 }

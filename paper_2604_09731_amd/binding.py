@@ -19,6 +19,7 @@ LIB_PATH = os.environ.get("SMART_TREE_LIB") or os.path.join(_HERE, "libsmart_tre
 SMART_OK, SMART_EINVAL, SMART_ETREE, SMART_ECAP, SMART_EHIP, SMART_ENOMEM = 0, -1, -2, -3, -4, -5
 SMART_F32, SMART_BF16 = 0, 1
 SMART_FP8_E4M3 = 2
+SMART_FP4_E2M1 = 3
 SMART_TVA_BAD_BLOCK = 1
 SMART_KV_PLAIN, SMART_KV_INTERLEAVED = 0, 1
 SMART_BEST_FIRST, SMART_LAYERWISE = 0, 1
@@ -33,7 +34,8 @@ EXPORTS = ["smart_strerror", "smart_last_hip_error", "smart_create", "smart_dest
            "smart_reserve", "smart_set_option", "smart_tva_profile_read", "smart_select_tree", "smart_select_tree_budgets", "smart_baseline_tree", "smart_product_forest", "smart_select_begin", "smart_select_layer",
            "smart_select_begin_device", "smart_select_layer_device", "tree_compact_pack", "tree_compact_pack_fill", "tree_rope", "smart_cost_tables", "smart_cost_tables_biased", "smart_fit_cost_models", "tree_upload",
            "tree_upload_pack", "tree_pack",
-           "kv_cache_write", "kv_cache_write_fp8", "tree_verify_attention", "tree_verify_attention_static", "tree_accept", "tree_accept_sample", "tree_commit", "tree_commit_fp8"]
+           "kv_cache_write", "kv_cache_write_fp8", "tree_verify_attention", "tree_verify_attention_static", "tree_accept", "tree_accept_sample", "tree_commit", "tree_commit_fp8",
+           "kv_cache_write_fp4", "kv_cache_read_fp4", "tree_commit_fp4", "prompt_attention"]
 
 
 class SmartError(RuntimeError):
@@ -61,6 +63,18 @@ class TvaParams(ctypes.Structure):
         ("h_cu_nodes", ctypes.c_void_p),
         ("k_scale", ctypes.c_float), ("v_scale", ctypes.c_float),
         ("d_status", ctypes.c_void_p),
+    ]
+
+
+class PromptParams(ctypes.Structure):
+    _fields_ = [
+        ("dtype", ctypes.c_int32), ("batch", ctypes.c_int32), ("total_tokens", ctypes.c_int32),
+        ("num_q_heads", ctypes.c_int32), ("num_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+        ("softmax_scale", ctypes.c_float),
+        ("d_q", ctypes.c_void_p), ("d_k", ctypes.c_void_p), ("d_v", ctypes.c_void_p),
+        ("q_stride", ctypes.c_int64), ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64),
+        ("out_stride", ctypes.c_int64),
+        ("d_cu_tokens", ctypes.c_void_p), ("d_out", ctypes.c_void_p), ("d_lse", ctypes.c_void_p),
     ]
 
 
@@ -155,6 +169,15 @@ def _lib():
         lib.tree_commit_fp8.restype = i32
         lib.tree_commit_fp8.argtypes = [vp, vp, i32, i32, i32, i32, i32, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp,
                                         vp, vp, vp, i64, i64, i64, vp, vp, ctypes.c_float, ctypes.c_float]
+        lib.kv_cache_write_fp4.restype = i32
+        lib.kv_cache_write_fp4.argtypes = [vp, vp, i32, i32, i32, i32, i32, i32, vp, vp, vp, vp, vp, i64, i64]
+        lib.kv_cache_read_fp4.restype = i32
+        lib.kv_cache_read_fp4.argtypes = [vp, vp, i32, i32, i32, i32, i32, i32, vp, vp, i64, i64, vp, vp, vp]
+        lib.tree_commit_fp4.restype = i32
+        lib.tree_commit_fp4.argtypes = [vp, vp, i32, i32, i32, i32, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp,
+                                        vp, vp, i64, i64, vp, vp]
+        lib.prompt_attention.restype = i32
+        lib.prompt_attention.argtypes = [vp, vp, ctypes.POINTER(PromptParams)]
         lib.tree_accept.restype = i32
         lib.tree_accept.argtypes = [vp, vp, i32, i32, vp, vp, vp, vp, vp, vp, vp]
         _libh = lib
@@ -386,7 +409,8 @@ _ROW = 128      # int32 elements
 
 _NATIVE_ENTRIES = ("smart_select_begin_device", "smart_select_layer_device", "tree_compact_pack_fill", "tree_upload_pack",
                    "tree_rope", "kv_cache_write", "kv_cache_write_fp8", "tree_verify_attention",
-                   "tree_verify_attention_static", "tree_accept", "tree_accept_sample", "tree_commit", "tree_commit_fp8")
+                   "tree_verify_attention_static", "tree_accept", "tree_accept_sample", "tree_commit", "tree_commit_fp8",
+                   "kv_cache_write_fp4", "kv_cache_read_fp4", "tree_commit_fp4", "prompt_attention")
 _nativeh = None
 
 
@@ -419,6 +443,11 @@ def _ptr(t):
     return t.data_ptr() if t is not None else None
 
 
+def _on_gpu(t):
+    if not t.is_cuda:       # (a kernel that reads host addresses faults)
+        raise ValueError(f"expected tensors on the GPU, got one on {t.device}")
+
+
 def _whole_rows(n):
     return (n + _ROW - 1) // _ROW * _ROW
 
@@ -436,6 +465,11 @@ def interleave_kv_cache(k_plain, v_plain):
     k = k_plain.reshape(nb, Hkv, bs, D // 8, 8).permute(0, 1, 3, 2, 4).contiguous()
     v = v_plain.reshape(nb, Hkv, bs // 8, 8, D).permute(0, 1, 2, 4, 3).contiguous()
     return k, v
+
+
+def fp4_page_bytes(block_size: int, head_dim: int) -> int:
+    """Bytes of a page (one block and kv head, of K or of V) of a 4-bit cache: the codes and the scale bytes behind them."""
+    return block_size * head_dim // 2 + block_size * head_dim // 32
 
 
 class SmartTree:
@@ -547,24 +581,55 @@ class SmartTree:
         self._native.cache_write(self._ctx, k_src, v_src, slot_mapping, k_cache, v_cache, layout, block_size, num_blocks,
                                  block_stride, head_stride, token_stride, True, k_scale, v_scale)
 
+    def kv_cache_write_fp4(self, k_src, v_src, slot_mapping, k_cache, v_cache, block_size):
+        """Rows [n, Hkv, D] into 4-bit caches: uint8 tensors [num_blocks, Hkv, fp4_page_bytes(block_size, D)]."""
+        _on_gpu(k_src)
+        self._native.cache_write_fp4(self._ctx, k_src, v_src, slot_mapping, k_cache, v_cache, block_size)
+
+    def kv_cache_read_fp4(self, slot_mapping, k_cache, v_cache, head_dim, block_size, dtype=None, k_out=None, v_out=None):
+        """The rows of the slots as values, (k, v) [n, Hkv, D] of ``dtype`` (default bfloat16; exact in float32 too);
+        zeros for slots that are negative or outside the cache."""
+        torch = _torch()
+        _on_gpu(k_cache)
+        shape = (slot_mapping.shape[0], k_cache.shape[1], int(head_dim))
+        k_out, v_out = (torch.empty(shape, dtype=dtype or torch.bfloat16, device=k_cache.device) if t is None else t
+                        for t in (k_out, v_out))
+        if tuple(k_out.shape) != shape:
+            raise ValueError(f"kv_cache_read_fp4: outputs must be {shape}")
+        self._native.cache_read_fp4(self._ctx, slot_mapping, k_cache, v_cache, block_size, k_out, v_out)
+        return k_out, v_out
+
+    # -- prompt_attention --------------------------------------------------
+    def prompt_attention(self, q, k, v, cu_tokens, softmax_scale, out=None, lse=None, want_lse=False):
+        """Causal attention of packed prompts: q [T, Hq, D], k and v [T, Hkv, D] (tokens may be strided, as parts of one
+        projection's output are), prompt b the tokens cu_tokens[b] .. cu_tokens[b + 1] - 1.  Returns out (like q,
+        contiguous unless given), or (out, lse [T, Hq]) if lse is given or wanted; rows of no prompt are not written."""
+        _on_gpu(q)
+        return self._native.prompt(self._ctx, q, k, v, cu_tokens, softmax_scale, out, lse, want_lse)
+
     # -- tree_verify_attention ---------------------------------------------
     def tree_verify_attention(self, q, k_tree, v_tree, k_cache, v_cache, block_table, prefix_len,
                               cu_nodes, anc_mask, softmax_scale, kv_layout, block_size=16,
                               out=None, lse=None, want_lse=False, h_cu_nodes=None, k_scale=None, v_scale=None,
-                              static=False, status=None):
+                              static=False, status=None, kv_cache_dtype=None):
         """k_cache / v_cache: [num_blocks, Hkv, ...] with one contiguous page of
         block_size * D elements per (block, head) (any of the two layouts).
         ``status``: optional int32 [B] tensor that receives the per-sequence block-table check.
         ``static``: call tree_verify_attention_static (no device allocation inside the library;
-        pass ``out`` / ``lse`` so that nothing is allocated here either)."""
+        pass ``out`` / ``lse`` so that nothing is allocated here either).
+        ``kv_cache_dtype``: SMART_FP4_E2M1 for 4-bit caches (uint8 [num_blocks, Hkv, fp4_page_bytes(block_size, D)],
+        kv_layout SMART_KV_INTERLEAVED); otherwise the tensors' type tells (uint8: fp8)."""
         h_address = 0
         if h_cu_nodes is not None:      # numpy int32 [B+1], host copy of cu_nodes
             h_cu_nodes = np.ascontiguousarray(h_cu_nodes, np.int32)
             assert h_cu_nodes.shape[0] == cu_nodes.shape[0]
             h_address = h_cu_nodes.ctypes.data
-        return self._native.attention(self._ctx, q, k_tree, v_tree, k_cache, v_cache, block_table, prefix_len, cu_nodes,
-                                      anc_mask, softmax_scale, kv_layout, block_size, out, lse, want_lse, h_address,
-                                      k_scale, v_scale, static, status)
+        if kv_cache_dtype not in (None, SMART_FP8_E4M3, SMART_FP4_E2M1):
+            raise ValueError(f"kv_cache_dtype {kv_cache_dtype!r}")
+        call = self._native.attention_fp4 if kv_cache_dtype == SMART_FP4_E2M1 else self._native.attention
+        return call(self._ctx, q, k_tree, v_tree, k_cache, v_cache, block_table, prefix_len, cu_nodes,
+                    anc_mask, softmax_scale, kv_layout, block_size, out, lse, want_lse, h_address, k_scale, v_scale, static,
+                    status)
 
     # -- tree_accept -------------------------------------------------------
     def tree_accept(self, cu_nodes, parent, token, target_next, max_depth):
@@ -584,3 +649,10 @@ class SmartTree:
         return self._native.commit(self._ctx, cu_nodes, accept_len, accept_path, k_tree, v_tree, k_cache, v_cache,
                                    block_table, prefix_len, layout, block_size, num_blocks, block_stride, head_stride,
                                    token_stride, k_scale, v_scale)
+
+    def tree_commit_fp4(self, cu_nodes, accept_len, accept_path, k_tree, v_tree, k_cache, v_cache, block_table, prefix_len,
+                        block_size):
+        """tree_commit into 4-bit caches (see kv_cache_write_fp4); returns (new_prefix_len, status)."""
+        _on_gpu(cu_nodes)
+        return self._native.commit_fp4(self._ctx, cu_nodes, accept_len, accept_path, k_tree, v_tree, k_cache, v_cache,
+                                       block_table, prefix_len, block_size)

@@ -5,6 +5,7 @@
 // dim), so that tree_verify_attention can load operands straight from HBM.
 #include "common.h"
 #include "fp8.h"
+#include "tree_commit.h"
 
 namespace {
 
@@ -258,8 +259,7 @@ static void launch_rows(hipStream_t s, int n_tokens, int Hkv, int D, int block_s
                      block_stride, head_stride, token_stride, k_scale, v_scale);
 }
 
-// One workgroup per (path index i, sequence b).  Every wavefront takes the same accept / refuse decision from the same
-// inputs (a lane per path entry: two memory round trips per 64 entries); workgroup i = 0 reports it.
+// One workgroup per (path index i, sequence b); workgroup i = 0 reports the sequence's verdict (commit_row).
 // kChunks: rows move in 8-element chunks (V of interleaved pages: four elements read at once, stored one by one); see
 // commit_in_chunks.  Four sequences, 8 kv heads of 128, max_depth 8, interleaved bf16: 4.0 us with a serial check of the
 // path, 3.6 with this one by element, 3.4 in chunks (start to end on the device).
@@ -275,27 +275,9 @@ __global__ __launch_bounds__(256) void tree_commit_kernel(
   const int i = blockIdx.x, b = blockIdx.y;
   const int lane = threadIdx.x & 63;
   const int base = cu_nodes[b];
-  const int n = cu_nodes[b + 1] - base;
-  const int a = accept_len[b];
-  const int start = prefix_len[b];
-  const int32_t* path = accept_path + (size_t)b * (max_depth + 1);
-  int verdict = SMART_OK, node = 0, block = 0;  // node, block: of path entry i
-  if (base < 0 || a < 0 || a > max_depth) {
-    verdict = SMART_ETREE;
-  } else if (start < 0 || (int64_t)start + a + 1 > (int64_t)max_blocks * block_size) {
-    verdict = SMART_ECAP;
-  } else {
-    for (int k0 = 0; k0 <= a; k0 += 64) {  // at most max_depth + 1 <= 129 entries
-      const int k = min(k0 + lane, a);
-      const int v = path[k];
-      const int blk = block_table[(size_t)b * max_blocks + (start + k) / block_size];
-      if (__any(v < 0 || v >= n || blk < 0 || blk >= num_blocks)) verdict = SMART_ETREE;
-      if (i >= k0 && i < k0 + 64) {
-        node = __builtin_amdgcn_readlane(v, i - k0);
-        block = __builtin_amdgcn_readlane(blk, i - k0);
-      }
-    }
-  }
+  const smart::CommitInputs in{max_depth, block_size, max_blocks, num_blocks, cu_nodes, accept_len, accept_path, block_table, prefix_len};
+  const smart::CommitRow row = smart::commit_row(in, i, b, base, cu_nodes[b + 1] - base, lane);
+  const int verdict = row.verdict, a = row.accepted, start = row.start, node = row.node, block = row.block;
   if (i == 0 && threadIdx.x == 0) {
     status[b] = verdict;
     new_prefix_len[b] = verdict == SMART_OK ? start + a + 1 : start;

@@ -29,6 +29,10 @@ struct Entries {
   decltype(&tree_accept_sample) sample;
   decltype(&tree_commit) commit;
   decltype(&tree_commit_fp8) commit_fp8;
+  decltype(&kv_cache_write_fp4) cache_write_fp4;
+  decltype(&kv_cache_read_fp4) cache_read_fp4;
+  decltype(&tree_commit_fp4) commit_fp4;
+  decltype(&prompt_attention) prompt;
 } lib;
 PyObject *check_call, *get_device, *raw_stream;
 
@@ -314,9 +318,172 @@ PyObject* cache_write(PyObject* const* a) {
   Py_RETURN_NONE;
 }
 
+// What the calls on 4-bit caches take from their tensors: [blocks, kv heads, bytes of a page] uint8, both of one shape.
+void page_bytes(const at::Tensor& kc, const at::Tensor& vc, int64_t kv_heads, int64_t block_size, int64_t head_dim) {
+  for (const at::Tensor* c : {&kc, &vc}) {
+    if (c->scalar_type() != at::kByte || c->dim() != 3 || c->size(1) != kv_heads || c->stride(2) != 1 ||
+        c->size(2) < SMART_FP4_PAGE_BYTES(block_size, head_dim) || c->size(0) != kc.size(0) || c->stride(0) != kc.stride(0) ||
+        c->stride(1) != kc.stride(1)) {
+      PyErr_SetString(PyExc_ValueError, "4-bit caches: two uint8 tensors [num_blocks, num_kv_heads, page bytes] of the same strides");
+      throw Failed();
+    }
+  }
+}
+void contiguous(const at::Tensor& t, const char* what) {
+  if (t.is_contiguous()) return;
+  PyErr_Format(PyExc_ValueError, "%s: rows must be contiguous", what);
+  throw Failed();
+}
+int32_t extent32(int64_t n) {
+  if (n <= INT32_MAX) return (int32_t)n;
+  PyErr_SetString(PyExc_ValueError, "a dimension does not fit 32 bits");
+  throw Failed();
+}
+void one_device(std::initializer_list<const at::Tensor*> ts) {
+  for (const at::Tensor* t : ts)
+    if (t->device() != (*ts.begin())->device()) {
+      PyErr_SetString(PyExc_ValueError, "tensors on different devices");
+      throw Failed();
+    }
+}
+void same_shape(const at::Tensor& a, const at::Tensor& b, const char* what) {
+  if (a.sizes() == b.sizes() && a.scalar_type() == b.scalar_type() && a.device() == b.device()) return;
+  PyErr_Format(PyExc_ValueError, "%s: shapes, element types or devices differ", what);
+  throw Failed();
+}
+void elements(const at::Tensor& t, at::ScalarType type, int64_t at_least, const char* what) {
+  if (t.scalar_type() == type && t.is_contiguous() && t.numel() >= at_least) return;
+  PyErr_Format(PyExc_ValueError, "%s: wrong element type, too short, or not contiguous", what);
+  throw Failed();
+}
+
+PyObject* cache_write_fp4(PyObject* const* a) {  // ctx, k_src, v_src, slots, k_cache, v_cache, block_size
+  auto ctx = pointer<smart_ctx>(a[0]);
+  const at::Tensor &k = tensor(a[1]), &v = tensor(a[2]), &slots = tensor(a[3]), &kc = tensor(a[4]), &vc = tensor(a[5]);
+  three_dims(k);
+  same_shape(k, v, "kv_cache_write_fp4");
+  contiguous(k, "kv_cache_write_fp4");
+  contiguous(v, "kv_cache_write_fp4");
+  elements(slots, at::kLong, k.size(0), "slot_mapping");
+  const int32_t n = extent32(k.size(0)), Hkv = extent32(k.size(1)), D = extent32(k.size(2)), type = element_type(k), bs = (int32_t)integer(a[6]);
+  page_bytes(kc, vc, Hkv, bs, D);
+  one_device({&k, &v, &slots, &kc, &vc});
+  const int32_t blocks_held = extent32(kc.size(0));
+  void* s = stream();
+  call("kv_cache_write_fp4", [&] {
+    return lib.cache_write_fp4(ctx, s, type, n, Hkv, D, bs, blocks_held, address(k), address(v), address<int64_t>(slots),
+                               address(kc), address(vc), kc.stride(0), kc.stride(1));
+  });
+  Py_RETURN_NONE;
+}
+
+PyObject* cache_read_fp4(PyObject* const* a) {  // ctx, slots, k_cache, v_cache, block_size, k_out, v_out
+  auto ctx = pointer<smart_ctx>(a[0]);
+  const at::Tensor &slots = tensor(a[1]), &kc = tensor(a[2]), &vc = tensor(a[3]), &k = tensor(a[5]), &v = tensor(a[6]);
+  three_dims(k);
+  same_shape(k, v, "kv_cache_read_fp4");
+  contiguous(k, "kv_cache_read_fp4");
+  contiguous(v, "kv_cache_read_fp4");
+  elements(slots, at::kLong, k.size(0), "slot_mapping");
+  const int32_t n = extent32(k.size(0)), Hkv = extent32(k.size(1)), D = extent32(k.size(2)), type = element_type(k), bs = (int32_t)integer(a[4]);
+  page_bytes(kc, vc, Hkv, bs, D);
+  one_device({&k, &v, &slots, &kc, &vc});
+  const int32_t blocks_held = extent32(kc.size(0));
+  void* s = stream();
+  call("kv_cache_read_fp4", [&] {
+    return lib.cache_read_fp4(ctx, s, type, n, Hkv, D, bs, blocks_held, address(kc), address(vc), kc.stride(0), kc.stride(1),
+                              address<int64_t>(slots), address(k), address(v));
+  });
+  Py_RETURN_NONE;
+}
+
+// ctx, cu_nodes, accept_len, accept_path, k_tree, v_tree, k_cache, v_cache, block_table, prefix_len, block_size
+PyObject* commit_fp4(PyObject* const* a) {
+  auto ctx = pointer<smart_ctx>(a[0]);
+  const at::Tensor &cu = tensor(a[1]), &length = tensor(a[2]), &path = tensor(a[3]), &kt = tensor(a[4]), &vt = tensor(a[5]),
+                   &kc = tensor(a[6]), &vc = tensor(a[7]), &table = tensor(a[8]), &prefix = tensor(a[9]);
+  three_dims(kt);
+  same_shape(kt, vt, "tree_commit_fp4");
+  contiguous(kt, "tree_commit_fp4");
+  contiguous(vt, "tree_commit_fp4");
+  const int32_t batch = extent32(extent(cu, 0) - 1), depth = extent32(extent(path, 1) - 1), Hkv = extent32(kt.size(1)),
+                D = extent32(kt.size(2)), type = element_type(kt), blocks = extent32(extent(table, 1)), bs = (int32_t)integer(a[10]);
+  elements(cu, at::kInt, (int64_t)batch + 1, "cu_nodes");
+  elements(length, at::kInt, batch, "accept_len");
+  elements(path, at::kInt, (int64_t)batch * (depth + 1), "accept_path");
+  elements(table, at::kInt, (int64_t)batch * blocks, "block_table");
+  elements(prefix, at::kInt, batch, "prefix_len");
+  page_bytes(kc, vc, Hkv, bs, D);
+  one_device({&kt, &vt, &kc, &vc, &cu, &length, &path, &table, &prefix});
+  auto rows = i32_rows(2, batch, cu);
+  const int32_t blocks_held = extent32(kc.size(0));
+  void* s = stream();
+  call("tree_commit_fp4", [&] {
+    return lib.commit_fp4(ctx, s, type, batch, depth, Hkv, D, bs, blocks, blocks_held, address<int32_t>(cu),
+                          address<int32_t>(length), address<int32_t>(path), address(kt), address(vt), address<int32_t>(table),
+                          address<int32_t>(prefix), address(kc), address(vc), kc.stride(0), kc.stride(1),
+                          address<int32_t>(rows[0]), address<int32_t>(rows[1]));
+  });
+  return tuple_of(rows[0], rows[1]);
+}
+
+// Tokens of [tokens, heads, head_dim] that need not lie one behind the other.
+int64_t token_stride(const at::Tensor& t, const char* what) {
+  three_dims(t);
+  const bool rows = (t.size(2) <= 1 || t.stride(2) == 1) && (t.size(1) <= 1 || t.stride(1) == t.size(2));
+  if (!rows) {
+    PyErr_Format(PyExc_ValueError, "%s: heads and head dims of a token must be contiguous", what);
+    throw Failed();
+  }
+  return t.size(0) > 1 ? t.stride(0) : t.size(1) * t.size(2);
+}
+
+PyObject* prompt(PyObject* const* a) {  // ctx, q, k, v, cu_tokens, scale, out, lse, want_lse
+  auto ctx = pointer<smart_ctx>(a[0]);
+  const at::Tensor &q = tensor(a[1]), &k = tensor(a[2]), &v = tensor(a[3]), &cu = tensor(a[4]);
+  prompt_params p = {};
+  p.q_stride = token_stride(q, "q");
+  p.k_stride = token_stride(k, "k");
+  p.v_stride = token_stride(v, "v");
+  same_shape(k, v, "prompt_attention");
+  p.dtype = element_type(q);
+  if (k.scalar_type() != q.scalar_type() || k.size(0) != q.size(0) || k.size(2) != q.size(2) || cu.dim() != 1) {
+    PyErr_SetString(PyExc_ValueError, "prompt_attention: q [T, Hq, D], k and v [T, Hkv, D] of one element type, cu_tokens [B + 1]");
+    throw Failed();
+  }
+  p.batch = extent32(extent(cu, 0) - 1);
+  elements(cu, at::kInt, 1, "cu_tokens");
+  p.total_tokens = extent32(q.size(0));
+  p.num_q_heads = extent32(q.size(1));
+  p.num_kv_heads = extent32(k.size(1));
+  p.head_dim = extent32(q.size(2));
+  p.softmax_scale = (float)real(a[5]);
+  at::Tensor out = a[6] == Py_None ? fresh(q, q.scalar_type(), q.sizes()) : tensor(a[6]), lse;
+  same_shape(q, out, "out");
+  p.out_stride = token_stride(out, "out");
+  if (a[7] != Py_None) {
+    lse = tensor(a[7]);
+    elements(lse, at::kFloat, q.size(0) * q.size(1), "lse");
+  } else if (truth(a[8])) {
+    lse = fresh(q, at::kFloat, {q.size(0), q.size(1)});
+  }
+  one_device({&q, &k, &v, &cu, &out});
+  if (lse.defined()) one_device({&q, &lse});
+  p.d_q = address(q);
+  p.d_k = address(k);
+  p.d_v = address(v);
+  p.d_cu_tokens = address<int32_t>(cu);
+  p.d_out = address(out);
+  p.d_lse = lse.defined() ? address<float>(lse) : nullptr;
+  void* s = stream();
+  call("prompt_attention", [&] { return lib.prompt(ctx, s, &p); });
+  return lse.defined() ? tuple_of(out, lse) : wrap(out);
+}
+
 // ctx, q, k_tree, v_tree, k_cache, v_cache, block_table, prefix_len, cu_nodes, anc_mask, scale, layout, block_size, out, lse,
 // want_lse, address of the host's offsets, k_scale, v_scale, static, status
-PyObject* attention(PyObject* const* a) {
+template <bool kFp4>
+PyObject* attention_over(PyObject* const* a) {
   auto ctx = pointer<smart_ctx>(a[0]);
   const at::Tensor &q = tensor(a[1]), &kt = tensor(a[2]), &vt = tensor(a[3]), &cu = tensor(a[8]);
   three_dims(q);
@@ -355,7 +522,10 @@ PyObject* attention(PyObject* const* a) {
       p.cache_token_stride = kc.stride(2);
     }
     p.d_block_table = address<int32_t>(tensor(a[6]));
-    if (kc.scalar_type() == at::kByte) {  // an fp8 (E4M3) cache
+    if (kFp4) {
+      page_bytes(kc, vc, p.num_kv_heads, p.block_size, p.head_dim);
+      p.kv_cache_dtype = SMART_FP4_E2M1;
+    } else if (kc.scalar_type() == at::kByte) {  // an fp8 (E4M3) cache
       p.kv_cache_dtype = SMART_FP8_E4M3;
       p.k_scale = (float)real(a[17]);
       p.v_scale = (float)real(a[18]);
@@ -378,6 +548,9 @@ PyObject* attention(PyObject* const* a) {
   else call("tree_verify_attention", [&] { return lib.attention(ctx, s, &p); });
   return lse.defined() ? tuple_of(out, lse) : wrap(out);
 }
+
+PyObject* attention(PyObject* const* a) { return attention_over<false>(a); }
+PyObject* attention_fp4(PyObject* const* a) { return attention_over<true>(a); }
 
 PyObject* accept(PyObject* const* a) {  // ctx, cu_nodes, parent, token, target_next, max_depth
   auto ctx = pointer<smart_ctx>(a[0]);
@@ -451,6 +624,8 @@ PyMethodDef methods[] = {SMART_METHOD(setup, 4),       SMART_METHOD(select_begin
                          SMART_METHOD(compact, 5),     SMART_METHOD(upload_pack, 5),
                          SMART_METHOD(rope, 7),        SMART_METHOD(cache_write, 15), SMART_METHOD(attention, 21),
                          SMART_METHOD(accept, 6),      SMART_METHOD(sample, 8),     SMART_METHOD(commit, 18),
+                         SMART_METHOD(attention_fp4, 21), SMART_METHOD(cache_write_fp4, 7), SMART_METHOD(cache_read_fp4, 7),
+                         SMART_METHOD(commit_fp4, 11), SMART_METHOD(prompt, 9),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef marshal_module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

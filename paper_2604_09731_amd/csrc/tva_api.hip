@@ -10,7 +10,8 @@ int32_t tva_check_params(const tva_params& p) {
   if (p.batch < 0 || p.total_nodes < 0 || p.num_q_heads <= 0 || p.num_kv_heads <= 0 ||
       p.num_q_heads % p.num_kv_heads != 0)
     return SMART_EINVAL;
-  if (p.kv_cache_dtype != 0 && p.kv_cache_dtype != SMART_FP8_E4M3) return SMART_EINVAL;
+  const bool fp4 = p.kv_cache_dtype == SMART_FP4_E2M1;
+  if (p.kv_cache_dtype != 0 && p.kv_cache_dtype != SMART_FP8_E4M3 && !fp4) return SMART_EINVAL;
   if (p.kv_cache_dtype == SMART_FP8_E4M3 &&
       (!(p.k_scale > 0.f) || !(p.k_scale < 3e38f) || !(p.v_scale > 0.f) || !(p.v_scale < 3e38f)))
     return SMART_EINVAL;
@@ -22,7 +23,11 @@ int32_t tva_check_params(const tva_params& p) {
   if ((int64_t)p.total_nodes * p.num_q_heads > 0x7FFFFFFF) return SMART_EINVAL;
   if (!(p.softmax_scale > 0.f) || !(p.softmax_scale < 1e30f)) return SMART_EINVAL;
   const int64_t page = (int64_t)p.block_size * p.head_dim;
-  if (p.kv_layout == SMART_KV_PLAIN) {
+  if (fp4) {
+    if (p.kv_layout != SMART_KV_INTERLEAVED || !fp4_cache_ok(p.block_size, p.head_dim, p.d_k_cache, p.d_v_cache, p.cache_block_stride,
+                                                            p.cache_head_stride))
+      return SMART_EINVAL;
+  } else if (p.kv_layout == SMART_KV_PLAIN) {
     if (p.cache_token_stride < p.head_dim) return SMART_EINVAL;
     if (p.cache_head_stride < (int64_t)(p.block_size - 1) * p.cache_token_stride + p.head_dim)
       return SMART_EINVAL;

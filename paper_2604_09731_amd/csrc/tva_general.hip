@@ -11,6 +11,7 @@
 #include <math.h>
 
 #include "common.h"
+#include "fp4.h"
 #include "fp8.h"
 
 namespace {
@@ -52,8 +53,27 @@ struct Layout {
   }
 };
 
-// T: element type of q, tree k / v and out; C: element type of the cache (T, or uint8_t = E4M3 whose
-// values are multiplied by k_scale / v_scale).
+// A cache of 4-bit elements (strides in bytes).
+struct Fp4 {
+  uint8_t byte;
+};
+template <typename C>
+__device__ inline float cached_k(const C* cache, const Layout& lay, int64_t blk, int g, int slot, int d) {
+  return to_float(cache[lay.k(blk, g, slot, d)]);
+}
+__device__ inline float cached_k(const Fp4* cache, const Layout& lay, int64_t blk, int g, int slot, int d) {
+  return smart::fp4_k_element(&cache->byte + blk * lay.block_stride + g * lay.head_stride, lay.block_size, lay.D, slot, d);
+}
+template <typename C>
+__device__ inline float cached_v(const C* cache, const Layout& lay, int64_t blk, int g, int slot, int d) {
+  return to_float(cache[lay.v(blk, g, slot, d)]);
+}
+__device__ inline float cached_v(const Fp4* cache, const Layout& lay, int64_t blk, int g, int slot, int d) {
+  return smart::fp4_v_element(&cache->byte + blk * lay.block_stride + g * lay.head_stride, lay.block_size, lay.D, slot, d);
+}
+
+// T: element type of q, tree k / v and out; C: element type of the cache (T, uint8_t = E4M3 whose values are multiplied by
+// k_scale / v_scale, or Fp4).
 template <typename T, typename C>
 __global__ __launch_bounds__(kWave) void tva_general_kernel(
     int batch, int total_nodes, int Hq, int Hkv, int D, int max_blocks, int num_blocks, float scale,
@@ -123,7 +143,7 @@ __global__ __launch_bounds__(kWave) void tva_general_kernel(
     if (valid) {
       float dot = 0.f;
       if (!tree) {
-        for (int d = 0; d < D; ++d) dot += s_q[d] * to_float(k_cache[lay.k(blk, g, slot, d)]);
+        for (int d = 0; d < D; ++d) dot += s_q[d] * cached_k(k_cache, lay, blk, g, slot, d);
         dot *= k_scale;
       } else {
         const T* kr = k_tree + ((size_t)(base + j) * Hkv + g) * D;
@@ -150,8 +170,8 @@ __global__ __launch_bounds__(kWave) void tva_general_kernel(
         int64_t vb = block_table[(size_t)b * max_blocks + t / lay.block_size];
         vb = vb < 0 ? 0 : (vb >= num_blocks ? num_blocks - 1 : vb);
         const int vs = t % lay.block_size;
-        if (lane < D) acc0 += pk * (v_scale * to_float(v_cache[lay.v(vb, g, vs, lane)]));
-        if (lane + kWave < D) acc1 += pk * (v_scale * to_float(v_cache[lay.v(vb, g, vs, lane + kWave)]));
+        if (lane < D) acc0 += pk * (v_scale * cached_v(v_cache, lay, vb, g, vs, lane));
+        if (lane + kWave < D) acc1 += pk * (v_scale * cached_v(v_cache, lay, vb, g, vs, lane + kWave));
       } else {
         const int jj = (c - n_prefix_chunks) * kWave + kk;
         const T* vr = v_tree + ((size_t)(base + jj) * Hkv + g) * D;
@@ -179,7 +199,7 @@ int32_t tva_launch_general(smart_ctx* ctx, hipStream_t stream, const tva_params&
              p.cache_token_stride};
   int32_t rc = profile_begin(ctx, stream);
   if (rc != SMART_OK) return rc;
-  const bool fp8 = p.kv_cache_dtype == SMART_FP8_E4M3;
+  const bool fp8 = p.kv_cache_dtype == SMART_FP8_E4M3, fp4 = p.kv_cache_dtype == SMART_FP4_E2M1;
   const float ks = fp8 ? p.k_scale : 1.f, vs = fp8 ? p.v_scale : 1.f;
 #define SMART_LAUNCH_GENERAL(T, C)                                                                            \
   hipLaunchKernelGGL((tva_general_kernel<T, C>), dim3((unsigned)rows), dim3(kWave), 0, stream, p.batch,      \
@@ -188,9 +208,9 @@ int32_t tva_launch_general(smart_ctx* ctx, hipStream_t stream, const tva_params&
                      (const T*)p.d_v_tree, (const C*)p.d_k_cache, (const C*)p.d_v_cache, p.d_block_table,    \
                      p.d_prefix_len, p.d_cu_nodes, p.d_anc_mask, (T*)p.d_out, p.d_lse, p.d_status)
   if (p.dtype == SMART_F32) {
-    if (fp8) SMART_LAUNCH_GENERAL(float, uint8_t); else SMART_LAUNCH_GENERAL(float, float);
+    if (fp4) SMART_LAUNCH_GENERAL(float, Fp4); else if (fp8) SMART_LAUNCH_GENERAL(float, uint8_t); else SMART_LAUNCH_GENERAL(float, float);
   } else {
-    if (fp8) SMART_LAUNCH_GENERAL(uint16_t, uint8_t); else SMART_LAUNCH_GENERAL(uint16_t, uint16_t);
+    if (fp4) SMART_LAUNCH_GENERAL(uint16_t, Fp4); else if (fp8) SMART_LAUNCH_GENERAL(uint16_t, uint8_t); else SMART_LAUNCH_GENERAL(uint16_t, uint16_t);
   }
 #undef SMART_LAUNCH_GENERAL
   SMART_HIP_CHECK(hipGetLastError());

@@ -44,6 +44,7 @@
 #include <math.h>
 
 #include "common.h"
+#include "fp4.h"
 #include "wave.h"
 
 namespace {
@@ -96,7 +97,7 @@ struct TiledArgs {
   int64_t block_stride, head_stride, token_stride;
   int32_t batch, total_nodes, Hq, Hkv, G, block_size, max_blocks, num_blocks;
   int32_t segment_cost;   // units of a segment beside its steps
-  bool fp8, plain;        // the cache's element type and layout, where they are no template arguments
+  bool fp8, fp4, plain;   // the cache's element type and layout, where they are no template arguments
   uint32_t block8_magic;  // token / 8 / (block_size / 8) by multiplication
   float scale;
   float c;         // softmax scale in powers of two (log2 e folded in)
@@ -250,8 +251,11 @@ __device__ inline int swizzle(int key) {
   return (((key >> 1) & 3) << 1) | ((key >> 3) & 1);
 }
 
-template <typename T, bool kFp8, bool kPlain, int D>
+enum CacheType { kSameType, kE4M3, kE2M1 };
+
+template <typename T, CacheType kCache, bool kPlain, int D>
 struct Stager {
+  static constexpr bool kFp8 = kCache == kE4M3;
   typedef typename RawChunk<T, kFp8>::type Raw;
   static constexpr int kE = 16 / (int)sizeof(T);          // elements per chunk
   static constexpr int kTileChunks = 4 * D;               // chunks of a tile's K (or V)
@@ -357,6 +361,114 @@ struct Stager {
 #pragma unroll
         for (int w = 0; w < 4; ++w) y[w] = w < keep ? y[w] : 0u;
         x = y;
+      }
+    }
+  }
+};
+
+// A 4-bit cache: a thread moves a 16-byte vector of a page (fp4.h), which becomes four (bf16) or eight (fp32) chunks in the
+// operand order of an interleaved page.
+__device__ inline bf16x8 bf16_of_codes(uint32_t w, float s) {  // eight codes of one scale, exactly
+  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 0), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 1);
+  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 2), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 3);
+  bf16x8 r;
+  r[0] = a[0]; r[1] = a[1]; r[2] = b[0]; r[3] = b[1];
+  r[4] = c[0]; r[5] = c[1]; r[6] = d[0]; r[7] = d[1];
+  return r;
+}
+// Four head dims of eight tokens -> a vector of the eight tokens for each head dim.  A conversion takes two head dims of one
+// token (one scale), a byte permutation then puts two tokens of one head dim together.
+__device__ inline void bf16_of_values(bf16x8 (&v)[4], uintx4 codes, uint64_t scales) {
+  uintx4 r[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {  // tokens 2 i and 2 i + 1
+    const float s0 = smart::fp4_scale((uint32_t)(scales >> (16 * i)) & 0xFFu), s1 = smart::fp4_scale((uint32_t)(scales >> (16 * i + 8)) & 0xFFu);
+    const uint32_t a01 = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[i], s0, 0));
+    const uint32_t a23 = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[i], s0, 1));
+    const uint32_t b01 = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[i], s1, 2));
+    const uint32_t b23 = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[i], s1, 3));
+    r[0][i] = __builtin_amdgcn_perm(b01, a01, 0x05040100u);
+    r[1][i] = __builtin_amdgcn_perm(b01, a01, 0x07060302u);
+    r[2][i] = __builtin_amdgcn_perm(b23, a23, 0x05040100u);
+    r[3][i] = __builtin_amdgcn_perm(b23, a23, 0x07060302u);
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) v[e] = __builtin_bit_cast(bf16x8, r[e]);
+}
+// Codes and scales of the first `keep` of a vector's eight tokens; the others become zeros.
+__device__ inline void keep_tokens(uintx4& codes, uint64_t& scales, int keep) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) codes[i] = keep >= 2 * i + 2 ? codes[i] : (keep == 2 * i + 1 ? codes[i] & 0xFFFFu : 0u);
+  scales = keep >= 8 ? scales : (keep <= 0 ? 0ull : scales & ((1ull << (8 * keep)) - 1ull));
+}
+
+template <typename T, int D>
+struct Stager<T, kE2M1, false, D> {
+  static constexpr int kTileChunks = 4 * D;
+  static constexpr int kStepChunks = kTilesPerStep * kTileChunks;
+  static constexpr int kKeys = TileKeys<T>::value;
+  static constexpr int kStepKeys = step_keys<T>();
+  static constexpr int kVectors = kStepKeys * D / 32;  // of K and of V in a step, at most one a thread
+  static_assert(kVectors <= kThreads, "one vector a thread");
+
+  int32_t idk, idv;
+  uintx4 k, v;
+  uint32_t ks;
+  uint64_t vs;
+
+  // What vector p of a step holds: of K, head dims 32 (p / kStepKeys) .. of one key; of V, four head dims of eight keys.
+  __device__ static int key_of_k(int p) { return p % kStepKeys; }
+  __device__ static int dim_of_k(int p) { return p / kStepKeys * 32; }
+  __device__ static int key_of_v(int p) { return p / (D / 4) * 8; }
+  __device__ static int dim_of_v(int p) { return p % (D / 4) * 4; }
+  __device__ static int block_of(const TiledArgs& a, int token) {
+    return (int)__umulhi(((uint32_t)token >> 3) << 1, a.block8_magic);
+  }
+  __device__ static int token_k(int step, int p, int len) { return min(step * kStepKeys + key_of_k(p), len - 1); }
+  __device__ static int token_v(int step, int p, int len) { return min(step * kStepKeys + key_of_v(p), (len - 1) & ~7); }
+
+  __device__ void load_ids(const TiledArgs& a, const int32_t* row, int step, int len, int tid) {
+    if (kVectors < kThreads && tid >= kVectors) return;
+    idk = row[block_of(a, token_k(step, tid, len))];
+    idv = row[block_of(a, token_v(step, tid, len))];
+  }
+  __device__ void load(const TiledArgs& a, int step, int len, int g, int tid) {
+    if (kVectors < kThreads && tid >= kVectors) return;
+    const int bs = a.block_size, tk = token_k(step, tid, len), tv = token_v(step, tid, len);
+    const int sk = tk - block_of(a, tk) * bs, sv = tv - block_of(a, tv) * bs;
+    const uint8_t* kp = (const uint8_t*)a.k_cache + clamp_block(idk, a.num_blocks) * a.block_stride + g * a.head_stride;
+    const uint8_t* vp = (const uint8_t*)a.v_cache + clamp_block(idv, a.num_blocks) * a.block_stride + g * a.head_stride;
+    k = *(const uintx4*)(kp + smart::fp4_k_vector(bs, sk, dim_of_k(tid)));
+    ks = kp[smart::fp4_k_scale(bs, D, sk, dim_of_k(tid))];
+    v = *(const uintx4*)(vp + smart::fp4_v_vector(D, sv, dim_of_v(tid)));
+    vs = *(const uint64_t*)(vp + smart::fp4_v_scale(bs, D, sv, dim_of_v(tid)));
+  }
+  // (as above: keys past `n_valid` get zeros as values)
+  __device__ void store(uintx4* lds, int tid, int n_valid) {
+    if (kVectors < kThreads && tid >= kVectors) return;
+    const int kk = key_of_k(tid), kd = dim_of_k(tid), vk = key_of_v(tid), vd = dim_of_v(tid);
+    if (n_valid - vk < 8) keep_tokens(v, vs, n_valid - vk);
+    const float s = smart::fp4_scale(ks);
+    bf16x8 x[4];
+    bf16_of_values(x, v, vs);
+    uintx4* kl = lds + kk / kKeys * kTileChunks;
+    uintx4* vl = lds + kStepChunks + vk / kKeys * kTileChunks;
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        kl[(kd / 8 + i) * 32 + kk % 32] = __builtin_bit_cast(uintx4, bf16_of_codes(k[i], s));
+        vl[(vk % kKeys / 8) * D + vd + i] = __builtin_bit_cast(uintx4, x[i]);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const floatx8 kf = __builtin_convertvector(bf16_of_codes(k[i], s), floatx8), vf = __builtin_convertvector(x[i], floatx8);
+        floatx4* kc = (floatx4*)kl + (kd / 8 + i) * 32 + kk % 16 * 2;
+        floatx4* vc = (floatx4*)vl + ((vk % kKeys / 8) * D + vd + i) * 2;
+        kc[0] = __builtin_shufflevector(kf, kf, 0, 1, 2, 3);
+        kc[1] = __builtin_shufflevector(kf, kf, 4, 5, 6, 7);
+        vc[0] = __builtin_shufflevector(vf, vf, 0, 1, 2, 3);
+        vc[1] = __builtin_shufflevector(vf, vf, 4, 5, 6, 7);
       }
     }
   }
@@ -791,6 +903,10 @@ struct Finish {
 #pragma unroll
         for (int k = 0; k < K4; ++k) {
           const int d = 4 * (e + 8 * k);  // four head dims of K, and of V in plain pages, lie together
+          if (a.fp4) {
+            cached4_fp4(k4[u][k], v4[u][k], (const uint8_t*)a.k_cache + page, (const uint8_t*)a.v_cache + page, a.block_size, slot, d);
+            continue;
+          }
           const int64_t row_at = page + slot * a.token_stride + d;
           k4[u][k] = cached4(a, a.k_cache, a.plain ? row_at : page + ((d >> 3) * a.block_size + slot) * 8 + (d & 7), false);
           v4[u][k] = cached4(a, a.v_cache, a.plain ? row_at : page + ((slot >> 3) * D + d) * 8 + (slot & 7), !a.plain);
@@ -833,6 +949,15 @@ struct Finish {
     for (int i = 0; i < 4; ++i) r[i] = (float)x[8 * i];
     return r;
   }
+  // Four head dims of one key of a 4-bit cache (two bytes of K's and of V's page).
+  __device__ static void cached4_fp4(floatx4& k, floatx4& v, const uint8_t* kp, const uint8_t* vp, int bs, int slot, int d) {
+    const uint32_t kw = *(const uint16_t*)(kp + smart::fp4_k_code(bs, slot, d)), vw = *(const uint16_t*)(vp + smart::fp4_v_code(D, slot, d));
+    const float ks = smart::fp4_scale(kp[smart::fp4_k_scale(bs, D, slot, d)]), vs = smart::fp4_scale(vp[smart::fp4_v_scale(bs, D, slot, d)]);
+    const floatx2 k0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(kw, ks, 0), k1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(kw, ks, 1);
+    const floatx2 v0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(vw, vs, 0), v1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(vw, vs, 1);
+    k = __builtin_shufflevector(k0, k1, 0, 1, 2, 3);
+    v = __builtin_shufflevector(v0, v1, 0, 1, 2, 3);
+  }
   __device__ void add_key(const floatx4 (&k4)[K4], const floatx4 (&v4)[K4], bool have, float k_scale, float v_scale, float c) {
     float x = 0.f;
     if (have) {
@@ -864,9 +989,9 @@ __device__ inline void zero_row(const TiledArgs& a, int64_t row, int e) {
 }
 
 // ---- the prefix kernel ----------------------------------------------------------------------------------------------------
-template <typename T, bool kFp8, bool kPlain, int D, bool kDirect>
+template <typename T, CacheType kCache, bool kPlain, int D, bool kDirect>
 __global__ __launch_bounds__(kThreads, 2) void tva_tiled_kernel(TiledArgs a) {
-  typedef Stager<T, kFp8, kPlain, D> Stage;
+  typedef Stager<T, kCache, kPlain, D> Stage;
   constexpr int kStepKeys = step_keys<T>();
   constexpr int kRegion = region_floats(D);
   constexpr int kStageBytes = 2 * 2 * Stage::kStepChunks * 16, kFoldBytes = kWaves * kRegion * 4;
@@ -1031,7 +1156,7 @@ __global__ __launch_bounds__(kThreads, 2) void tva_tiled_kernel(TiledArgs a) {
           for (int x = first; x < kTilesPerStep; x += shared) {
             const int n_valid = len - t * kStepKeys - x * Stage::kKeys;
             if (n_valid <= 0) break;
-            rowset.template tile<!kFp8>(stage + x * Stage::kTileChunks, stage + Stage::kStepChunks + x * Stage::kTileChunks, n_valid,
+            rowset.template tile<kCache == kSameType>(stage + x * Stage::kTileChunks, stage + Stage::kStepChunks + x * Stage::kTileChunks, n_valid,
                                         a.c_stored, lane);
           }
       }
@@ -1237,6 +1362,9 @@ size_t tva_tiled_reserve(const smart_ctx* ctx, int32_t batch, int32_t total_node
 // Every 16-byte chunk of a staged row, every query row and every tree row must be addressable with one load.
 bool tva_tiled_supported(const tva_params& p) {
   const bool fp8 = p.kv_cache_dtype == SMART_FP8_E4M3;
+  if (p.kv_cache_dtype == SMART_FP4_E2M1)  // (its pages are aligned: tva_check_params)
+    return p.max_blocks_per_seq > 0 && p.num_blocks > 0 && (((uintptr_t)p.d_q | (uintptr_t)p.d_k_tree | (uintptr_t)p.d_v_tree |
+                                                            (uintptr_t)p.d_out) & 15u) == 0;
   const int chunk = p.dtype == SMART_F32 ? 4 : 8;                            // elements
   const uintptr_t cache_align = fp8 ? (uintptr_t)chunk : 16;                 // bytes
   auto aligned = [](const void* x, uintptr_t n) { return ((uintptr_t)x & (n - 1)) == 0; };
@@ -1273,18 +1401,18 @@ static void launch_finish(const TiledArgs& a, int64_t rows8, hipStream_t stream)
   else hipLaunchKernelGGL((tva_tiled_finish_kernel<T, D, 0>), grid, block, 0, stream, a);
 }
 
-template <typename T, bool kFp8, bool kPlain, int D>
+template <typename T, CacheType kCache, bool kPlain, int D>
 static hipError_t launch_tiled(const TiledArgs& a, bool direct, unsigned grid, hipStream_t stream) {
   if (direct)
-    hipLaunchKernelGGL((tva_tiled_kernel<T, kFp8, kPlain, D, true>), dim3(grid), dim3(kThreads), 0, stream, a);
+    hipLaunchKernelGGL((tva_tiled_kernel<T, kCache, kPlain, D, true>), dim3(grid), dim3(kThreads), 0, stream, a);
   else
-    hipLaunchKernelGGL((tva_tiled_kernel<T, kFp8, kPlain, D, false>), dim3(grid), dim3(kThreads), 0, stream, a);
+    hipLaunchKernelGGL((tva_tiled_kernel<T, kCache, kPlain, D, false>), dim3(grid), dim3(kThreads), 0, stream, a);
   return hipGetLastError();
 }
 
 int32_t tva_launch_tiled(smart_ctx* ctx, hipStream_t stream, const tva_params& p, const TvaWorkspace* fixed) {
   const int G = p.num_q_heads / p.num_kv_heads;
-  const bool fp8 = p.kv_cache_dtype == SMART_FP8_E4M3, f32 = p.dtype == SMART_F32;
+  const bool fp8 = p.kv_cache_dtype == SMART_FP8_E4M3, fp4 = p.kv_cache_dtype == SMART_FP4_E2M1, f32 = p.dtype == SMART_F32;
   const int64_t segs = tiled_segments(p.batch, p.total_nodes, p.num_q_heads, p.num_kv_heads);
   const int64_t rows8 = ((int64_t)p.total_nodes * p.num_q_heads + kWave / kCombineLanes - 1) / (kWave / kCombineLanes);
   if (segs > 0x7FFFFFFF) return SMART_EINVAL;
@@ -1348,6 +1476,7 @@ int32_t tva_launch_tiled(smart_ctx* ctx, hipStream_t stream, const tva_params& p
   a.num_blocks = p.num_blocks;
   a.segment_cost = segment_cost(p, tiled_workgroups(ctx));
   a.fp8 = fp8;
+  a.fp4 = fp4;
   a.plain = p.kv_layout == SMART_KV_PLAIN;
   // t8 / d as the high word of 2 t8 * (floor(2^31 / d) + 1): exact for t8 < 2^28 and d <= 8
   a.block8_magic = (uint32_t)((1ull << 31) / ((uint32_t)p.block_size / 8)) + 1u;
@@ -1362,14 +1491,16 @@ int32_t tva_launch_tiled(smart_ctx* ctx, hipStream_t stream, const tva_params& p
   const unsigned grid = direct ? (unsigned)segs : (unsigned)tiled_workgroups(ctx);
   const bool plain = a.plain;
   hipError_t err = hipErrorInvalidValue;
-#define SMART_TILED(T, FP8, PLAIN) \
-  err = p.head_dim == 128 ? launch_tiled<T, FP8, PLAIN, 128>(a, direct, grid, stream) : launch_tiled<T, FP8, PLAIN, 64>(a, direct, grid, stream)
+#define SMART_TILED(T, CACHE, PLAIN) \
+  err = p.head_dim == 128 ? launch_tiled<T, CACHE, PLAIN, 128>(a, direct, grid, stream) : launch_tiled<T, CACHE, PLAIN, 64>(a, direct, grid, stream)
   if (f32) {
-    if (fp8) { if (plain) SMART_TILED(float, true, true); else SMART_TILED(float, true, false); }
-    else { if (plain) SMART_TILED(float, false, true); else SMART_TILED(float, false, false); }
+    if (fp4) SMART_TILED(float, kE2M1, false);
+    else if (fp8) { if (plain) SMART_TILED(float, kE4M3, true); else SMART_TILED(float, kE4M3, false); }
+    else { if (plain) SMART_TILED(float, kSameType, true); else SMART_TILED(float, kSameType, false); }
   } else {
-    if (fp8) { if (plain) SMART_TILED(__bf16, true, true); else SMART_TILED(__bf16, true, false); }
-    else { if (plain) SMART_TILED(__bf16, false, true); else SMART_TILED(__bf16, false, false); }
+    if (fp4) SMART_TILED(__bf16, kE2M1, false);
+    else if (fp8) { if (plain) SMART_TILED(__bf16, kE4M3, true); else SMART_TILED(__bf16, kE4M3, false); }
+    else { if (plain) SMART_TILED(__bf16, kSameType, true); else SMART_TILED(__bf16, kSameType, false); }
   }
 #undef SMART_TILED
   SMART_HIP_CHECK(err);
