@@ -29,6 +29,11 @@ __device__ inline int fp4_v_scale(int bs, int D, int slot, int d) { return bs * 
 // A scale byte as the binary32 the conversions take its exponent from.
 __device__ inline float fp4_scale(uint32_t byte) { return __uint_as_float(byte << 23); }
 
+// The same out of byte kByte of a dword, with what lies beside the byte left where it is: the conversions look at the exponent
+// bits alone (checked for all bytes against 256 patterns of sign and mantissa bits).
+template <int kByte>
+__device__ inline float fp4_scale_of(uint32_t w) { return __uint_as_float(kByte == 3 ? w >> 1 : w << (23 - 8 * kByte)); }
+
 // One element of a page, as binary32 (exact).
 __device__ inline float fp4_element(uint8_t pair, uint8_t scale, int d) {
   const fp4_floatx2 x = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4((uint32_t)pair, fp4_scale(scale), 0);

@@ -382,7 +382,8 @@ __device__ inline void bf16_of_values(bf16x8 (&v)[4], uintx4 codes, uint64_t sca
   uintx4 r[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {  // tokens 2 i and 2 i + 1
-    const float s0 = smart::fp4_scale((uint32_t)(scales >> (16 * i)) & 0xFFu), s1 = smart::fp4_scale((uint32_t)(scales >> (16 * i + 8)) & 0xFFu);
+    const uint32_t w = (uint32_t)(scales >> (32 * (i >> 1)));
+    const float s0 = i & 1 ? smart::fp4_scale_of<2>(w) : smart::fp4_scale_of<0>(w), s1 = i & 1 ? smart::fp4_scale_of<3>(w) : smart::fp4_scale_of<1>(w);
     const uint32_t a01 = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[i], s0, 0));
     const uint32_t a23 = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[i], s0, 1));
     const uint32_t b01 = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[i], s1, 2));
@@ -524,7 +525,7 @@ struct Rows<__bf16, kPlain, D> {
   }
   __device__ static int key_of_row(int i) { return kPlain ? i : (i & 16) + sigma(i & 15); }
 
-  template <bool kInPlace>
+  template <bool kInPlace, bool kOnePart>
   __device__ void tile(const uintx4* kt, const uintx4* vt, int n_valid, float c, int lane) {
     const int h = lane >> 5, j = lane & 31;
     const int key = key_of_row(j);
@@ -567,6 +568,11 @@ struct Rows<__bf16, kPlain, D> {
       l += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
       // p = hi + mid + lo exactly: three bf16 values hold the 24 bits of a binary32
       const bf16x8 hi = __builtin_convertvector(p, bf16x8);
+      if (kOnePart) {
+#pragma unroll
+        for (int jt = 0; jt < D / 32; ++jt) o[jt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[kk][jt], hi, o[jt], 0, 0, 0);
+        continue;
+      }
       const floatx8 r1 = p - unpacked<kInPlace>(hi);
       const bf16x8 mid = __builtin_convertvector(r1, bf16x8);
       const bf16x8 lo = __builtin_convertvector(r1 - unpacked<kInPlace>(mid), bf16x8);
@@ -642,7 +648,7 @@ struct Rows<float, kPlain, D> {
       l[nh] = 0.f;
     }
   }
-  template <bool kInPlace>
+  template <bool kInPlace, bool kOnePart>
   __device__ void tile(const uintx4* kt, const uintx4* vt, int n_valid, float c, int lane) {
     const int quarter = lane >> 4, i = lane & 15;
     floatx4 s[2] = {(floatx4)(0.f), (floatx4)(0.f)};
@@ -740,6 +746,174 @@ struct Rows<float, kPlain, D> {
         region[kRowTile * D + row] = m[nh];
         region[kRowTile * D + kRowTile + row] = sum;
       }
+    }
+  }
+};
+
+// ---- a 4-bit cache and few rows: operands straight from the pages -----------------------------------------------------------
+// One wavefront's 32 rows against tiles of 32 keys, head dim 128.  A lane's 16-byte vectors are its operands: of K, 32 head dims
+// of one key (the queries are laid out in the same order of the contraction); of V, four head dims of eight keys, a vector of
+// keys for each of the four output tiles (tile jt holds head dims 4 m + jt).  Nothing is shared between wavefronts, so nothing
+// goes through LDS and a wavefront keeps two tiles of its own in flight.
+// A probability is rounded to bf16 for the output product, as on the interleaved bf16 path (off by 2^-9 of itself at most, a
+// quarter of what the result's own rounding may cost; a second part would take 40 of a tile's vector instructions).
+struct Fp4Stream {
+  static constexpr int D = 128;
+  struct Ids {  // block and slot / 8 in it of the group of eight keys that a lane's K, V and V vectors belong to
+    int32_t k, v[2];
+    int32_t ks, vs[2];
+  };
+  struct Raw {
+    uintx4 k[2], v[2];
+    uint32_t ks;
+    uint64_t vs[2];
+  };
+  bf16x8 q[D / 16];
+  floatx16 o[D / 32];
+  float m, l;  // of row lane % 32; l: this half-wavefront's keys
+
+  __device__ void begin(const TiledArgs& a, int base, int g, int row0, int rows, int lane) {
+    const int h = lane >> 5, j = lane & 31;
+    const int rho = min(row0 + j, rows - 1);  // padding rows repeat the last real row; never read back
+    const int node = base + rho / a.G, head = g * a.G + rho % a.G;
+    const __bf16* qp = (const __bf16*)a.q + ((int64_t)node * a.Hq + head) * D + 32 * h;
+#pragma unroll
+    for (int c = 0; c < 2; ++c)
+#pragma unroll
+      for (int w = 0; w < 4; ++w) q[4 * c + w] = *(const bf16x8*)(qp + 64 * c + 8 * w);
+#pragma unroll
+    for (int jt = 0; jt < D / 32; ++jt) o[jt] = (floatx16)(0.f);
+    m = -INFINITY;
+    l = 0.f;
+  }
+  // Row i of the score tile holds key (i & 16) + sigma(i & 15) of the tile: a lane's eight registers are eight consecutive keys.
+  // Groups of eight keys lie in one page, so what a vector holds behind the prefix's end is in the page too (and masked);
+  // groups behind the one that the prefix ends in become that one.
+  __device__ static int group_of_k(int lane) { return ((lane & 16) + sigma(lane & 15)) >> 3; }
+  __device__ static void load_id(int32_t& id, int32_t& slot8, const TiledArgs& a, const int32_t* row, int group) {
+    const uint32_t block = __umulhi((uint32_t)group << 1, a.block8_magic);
+    slot8 = group - (int)block * (a.block_size >> 3);
+    id = row[block];
+  }
+  __device__ static void load_ids(Ids& id, const TiledArgs& a, const int32_t* row, int tile, int len, int lane) {
+    const int last = (len - 1) >> 3;
+    load_id(id.k, id.ks, a, row, min(tile * 4 + group_of_k(lane), last));
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk) load_id(id.v[kk], id.vs[kk], a, row, min(tile * 4 + 2 * kk + (lane >> 5), last));
+  }
+  // (the stride of a block fits 32 bits: tva_tiled_supported)
+  __device__ static const uint8_t* page_of(const TiledArgs& a, const uint8_t* cache, int32_t id) {
+    return cache + (uint64_t)(uint32_t)min(max(id, 0), a.num_blocks - 1) * (uint32_t)a.block_stride;
+  }
+  __device__ static void load(Raw& r, const Ids& id, const TiledArgs& a, const uint8_t* kc, const uint8_t* vc, int lane) {
+    const int bs = a.block_size, h = lane >> 5, in8 = sigma(lane & 15) & 7, d = 4 * (lane & 31);
+    const uint8_t* kp = page_of(a, kc, id.k);
+    const uint32_t k_at = (uint32_t)(id.ks * 128 + (h * bs + in8) * 16);
+    r.k[0] = *(const uintx4*)(kp + k_at);
+    r.k[1] = *(const uintx4*)(kp + (k_at + 32u * bs));
+    r.ks = *(const uint32_t*)(kp + (uint32_t)(id.ks * 32 + bs * (D / 2) + in8 * 4));
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk) {
+      const uint8_t* vp = page_of(a, vc, id.v[kk]);
+      r.v[kk] = *(const uintx4*)(vp + (uint32_t)(id.vs[kk] * (4 * D) + d * 4));
+      r.vs[kk] = *(const uint64_t*)(vp + (uint32_t)(id.vs[kk] * 8 + bs * (D / 2) + (d >> 5) * bs));
+    }
+  }
+  template <bool kMask>
+  __device__ void tile(Raw& r, int n_valid, float c, int lane) {
+    const int h = lane >> 5;
+    const uint32_t ks = r.ks >> (8 * h);
+    floatx16 s = (floatx16)(0.f);
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      const float sc = x == 0 ? smart::fp4_scale_of<0>(ks) : smart::fp4_scale_of<2>(ks);
+#pragma unroll
+      for (int w = 0; w < 4; ++w) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(bf16_of_codes(r.k[x][w], sc), q[4 * x + w], s, 0, 0, 0);
+    }
+    if (kMask && n_valid < 32) {
+      const int left = n_valid - 8 * h;  // register i: key 16 (i / 8) + 8 h + i % 8
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (16 * (i >> 3) + (i & 7) >= left) s[i] = -INFINITY;
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk) keep_tokens(r.v[kk], r.vs[kk], left - 16 * kk);
+    }
+    float mx = s[0];
+#pragma unroll
+    for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[i]);
+    mx = max_halves(mx);
+    const float m_new = fmaxf(m, mx);
+    if (__any((m_new - m) * c > kRescaleStep)) {
+      const float alpha = weight(m, m_new, c);
+      l *= alpha;
+#pragma unroll
+      for (int jt = 0; jt < D / 32; ++jt) o[jt] *= alpha;
+      m = m_new;
+    }
+    const float mc = m == -INFINITY ? 0.f : m * c;
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk) {
+      floatx8 p;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) p[e] = __builtin_amdgcn_exp2f(fmaf(s[8 * kk + e], c, -mc));
+      l += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
+      const bf16x8 pb = __builtin_convertvector(p, bf16x8);
+      bf16x8 v[4];
+      bf16_of_values(v, r.v[kk], r.vs[kk]);
+#pragma unroll
+      for (int jt = 0; jt < D / 32; ++jt) o[jt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[jt], pb, o[jt], 0, 0, 0);
+    }
+  }
+  // Tiles first, first + stride, .. below `end` of the prefix.  (Requests past the end ask for the last tile again: a branch
+  // would make every wait one for everything in flight.)
+  __device__ void run(const TiledArgs& a, const int32_t* table, int g, int first, int end, int stride, int len, int lane) {
+    if (first >= end) return;
+    const uint8_t* kc = (const uint8_t*)a.k_cache + (int64_t)g * a.head_stride;
+    const uint8_t* vc = (const uint8_t*)a.v_cache + (int64_t)g * a.head_stride;
+    Ids id[2];
+    Raw raw[2];
+    // (The barriers keep the order of the requests: a wait then leaves the younger ones in flight.)
+    auto request_ids = [&](int u, int t) {
+      load_ids(id[u], a, table, min(t, end - 1), len, lane);
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    auto request = [&](int u, int t) {  // ids of tile t are there; asks for those of the tile after the next one
+      load(raw[u], id[u], a, kc, vc, lane);
+      __builtin_amdgcn_sched_barrier(0);
+      request_ids(u, t + 2 * stride);
+    };
+    request_ids(0, first);
+    request_ids(1, first + stride);
+    request(0, first);
+    request(1, first + stride);
+    // All but the last one or two in pairs (no way out of a pair: where one can be left between its tiles, the waits of both
+    // are for everything in flight).  Only the wavefront's last tile can be the one that the prefix ends in.
+    const int pairs = ((end - 1 - first) / stride) / 2;
+    int x = first;
+    for (int i = 0; i < pairs; ++i, x += 2 * stride) {
+      tile<false>(raw[0], 32, a.c_stored, lane);
+      request(0, x + 2 * stride);
+      tile<false>(raw[1], 32, a.c_stored, lane);
+      request(1, x + 3 * stride);
+    }
+    tile<true>(raw[0], len - x * 32, a.c_stored, lane);
+    x += stride;
+    if (x < end) tile<true>(raw[1], len - x * 32, a.c_stored, lane);
+  }
+  // The state in LDS as Rows::put lays it down.
+  __device__ void put(float* region, int lane) {
+    const int h = lane >> 5, j = lane & 31;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      floatx4 x;
+#pragma unroll
+      for (int jt = 0; jt < 4; ++jt) x[jt] = o[jt][i];
+      ((floatx4*)region)[(8 * (i >> 2) + 4 * h + (i & 3)) * kRowTile + j] = x;
+    }
+    const float sum = sum_halves(l);
+    if (h == 0) {
+      region[kRowTile * D + j] = m;
+      region[kRowTile * D + kRowTile + j] = sum;
     }
   }
 };
@@ -1130,40 +1304,52 @@ __global__ __launch_bounds__(kThreads, 2) void tva_tiled_kernel(TiledArgs a) {
       const int r = (group_rows + kRowTile - 1) / kRowTile;
       // row tile, first tile of a step and stride between tiles of this wavefront; wavefronts rt, rt + apart, ... share one
       const int apart = r >= 3 ? 4 : r;
-      const int shared = r >= 3 ? 2 : 4;  // wavefronts per row tile
+      // a 4-bit cache and one row tile: every wavefront streams tiles of its own
+      const bool stream = kCache == kE2M1 && sizeof(T) == 2 && D == 128 && r == 1;
+      const int shared = stream ? kWaves : (r >= 3 ? 2 : 4);  // wavefronts per row tile
       const int rt = wv & (apart - 1), first = r == 1 ? wv : (r == 2 ? wv >> 1 : wv >> 2);
       const bool busy = rt < r && first < kTilesPerStep;
-
-      Rows<T, kPlain, D> rowset;
-      rowset.begin(a, sh.base, g, row0 + (busy ? rt * kRowTile : 0), rows, lane);
       const int32_t* table = a.block_table + (int64_t)b * a.max_blocks;
-      Stage st;
-      if (t0 < t1) {
-        st.load_ids(a, table, t0, len, tid);
-        st.load(a, t0, len, g, tid);
-        if (t0 + 1 < t1) st.load_ids(a, table, t0 + 1, len, tid);
-      }
-      __syncthreads();  // the piece before is done with the LDS
-      for (int t = t0; t < t1; ++t) {
-        uintx4* stage = lds + (t & 1) * (2 * Stage::kStepChunks);
-        st.store(stage, tid, len - t * kStepKeys);
-        if (t + 1 < t1) {
-          st.load(a, t + 1, len, g, tid);
-          if (t + 2 < t1) st.load_ids(a, table, t + 2, len, tid);
-        }
-        __syncthreads();  // the stage is full, and everyone is done with the other one
-        if (busy)
-          for (int x = first; x < kTilesPerStep; x += shared) {
-            const int n_valid = len - t * kStepKeys - x * Stage::kKeys;
-            if (n_valid <= 0) break;
-            rowset.template tile<kCache == kSameType>(stage + x * Stage::kTileChunks, stage + Stage::kStepChunks + x * Stage::kTileChunks, n_valid,
-                                        a.c_stored, lane);
-          }
-      }
-      // fold: the states that share a row tile, in wavefront order
-      __syncthreads();
       float* regions = (float*)lds;
-      rowset.put(regions + wv * kRegion, lane);
+      if constexpr (kCache == kE2M1 && sizeof(T) == 2 && D == 128) {
+        if (stream) {
+          Fp4Stream st;
+          st.begin(a, sh.base, g, row0, rows, lane);
+          st.run(a, table, g, t0 * kTilesPerStep + wv, min(t1 * kTilesPerStep, (len + 31) / 32), kWaves, len, lane);
+          __syncthreads();  // the piece before is done with the LDS
+          st.put(regions + wv * kRegion, lane);
+        }
+      }
+      if (!stream) {
+        Rows<T, kPlain, D> rowset;
+        rowset.begin(a, sh.base, g, row0 + (busy ? rt * kRowTile : 0), rows, lane);
+        Stage st;
+        if (t0 < t1) {
+          st.load_ids(a, table, t0, len, tid);
+          st.load(a, t0, len, g, tid);
+          if (t0 + 1 < t1) st.load_ids(a, table, t0 + 1, len, tid);
+        }
+        __syncthreads();  // the piece before is done with the LDS
+        for (int t = t0; t < t1; ++t) {
+          uintx4* stage = lds + (t & 1) * (2 * Stage::kStepChunks);
+          st.store(stage, tid, len - t * kStepKeys);
+          if (t + 1 < t1) {
+            st.load(a, t + 1, len, g, tid);
+            if (t + 2 < t1) st.load_ids(a, table, t + 2, len, tid);
+          }
+          __syncthreads();  // the stage is full, and everyone is done with the other one
+          if (busy)
+            for (int x = first; x < kTilesPerStep; x += shared) {
+              const int n_valid = len - t * kStepKeys - x * Stage::kKeys;
+              if (n_valid <= 0) break;
+              rowset.template tile<kCache == kSameType, kCache == kE2M1>(stage + x * Stage::kTileChunks, stage + Stage::kStepChunks + x * Stage::kTileChunks, n_valid,
+                                          a.c_stored, lane);
+            }
+        }
+        // fold: the states that share a row tile, in wavefront order
+        __syncthreads();
+        rowset.put(regions + wv * kRegion, lane);
+      }
       __syncthreads();
       float* slot = kDirect ? nullptr : a.ws + (wg + at.segs_before + (int64_t)g * sh.groups + group) * slot_floats(D);
       if (tid < r * kRowTile) {
@@ -1362,8 +1548,8 @@ size_t tva_tiled_reserve(const smart_ctx* ctx, int32_t batch, int32_t total_node
 // Every 16-byte chunk of a staged row, every query row and every tree row must be addressable with one load.
 bool tva_tiled_supported(const tva_params& p) {
   const bool fp8 = p.kv_cache_dtype == SMART_FP8_E4M3;
-  if (p.kv_cache_dtype == SMART_FP4_E2M1)  // (its pages are aligned: tva_check_params)
-    return p.max_blocks_per_seq > 0 && p.num_blocks > 0 && (((uintptr_t)p.d_q | (uintptr_t)p.d_k_tree | (uintptr_t)p.d_v_tree |
+  if (p.kv_cache_dtype == SMART_FP4_E2M1)  // (its pages are aligned: tva_check_params; the streams multiply 32-bit strides)
+    return p.cache_block_stride < (int64_t)1 << 32 && p.max_blocks_per_seq > 0 && p.num_blocks > 0 && (((uintptr_t)p.d_q | (uintptr_t)p.d_k_tree | (uintptr_t)p.d_v_tree |
                                                             (uintptr_t)p.d_out) & 15u) == 0;
   const int chunk = p.dtype == SMART_F32 ? 4 : 8;                            // elements
   const uintptr_t cache_align = fp8 ? (uintptr_t)chunk : 16;                 // bytes
