@@ -16,18 +16,19 @@ def prompt_attention(q, k, v, cu, scale):
     G = Hq // k.shape[1]
     out, mean_abs = np.full((T, Hq, D), np.nan), np.full((T, Hq, D), np.nan)
     lse, size = np.full((T, Hq), np.nan), np.full((T, Hq), np.nan)
-    with np.errstate(invalid="ignore", over="ignore"):
-        for lo, hi in zip(cu[:-1], cu[1:]):
+    for lo, hi in zip(cu[:-1], cu[1:]):
+        for t in range(lo, hi):
             for h in range(Hq):
-                g = h // G
-                for t in range(lo, hi):
-                    keys, values = k[lo:t + 1, g], v[lo:t + 1, g]
-                    s = scale * (keys @ q[t, h])
-                    m = s.max()
-                    p = np.exp(s - m)
-                    w = p / p.sum()
-                    out[t, h] = w @ values
-                    mean_abs[t, h] = w @ np.abs(values)
-                    lse[t, h] = m + np.log(p.sum())
-                    size[t, h] = scale * (np.abs(keys) @ np.abs(q[t, h])).max()
+                out[t, h], lse[t, h], mean_abs[t, h], size[t, h] = prompt_row(q[t, h], k[lo:t + 1, h // G], v[lo:t + 1, h // G],
+                                                                              scale)
     return out, lse, mean_abs, size
+
+
+def prompt_row(q, keys, values, scale):
+    """One row over its own keys: its output, log-sum-exp, average of |v| and largest sum |q| |k|."""
+    with np.errstate(invalid="ignore", over="ignore"):
+        s = scale * (keys @ q)
+        m = s.max()
+        p = np.exp(s - m)
+        w = p / p.sum()
+        return w @ values, m + np.log(p.sum()), w @ np.abs(values), scale * (np.abs(keys) @ np.abs(q)).max()

@@ -19,6 +19,7 @@ namespace {
 
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
 typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 typedef __attribute__((ext_vector_type(4))) short shortx4;
 typedef __attribute__((ext_vector_type(4))) float floatx4;
 typedef __attribute__((ext_vector_type(8))) float floatx8;
@@ -27,12 +28,12 @@ typedef __attribute__((ext_vector_type(4))) uint32_t uintx4;
 typedef __attribute__((address_space(3))) shortx4 lds_shortx4;
 
 constexpr int kWave = 64;
-constexpr int kWaves = 4;
-constexpr int kThreads = kWave * kWaves;
 constexpr int kTile = 32;  // keys and rows of a score tile
 constexpr float kLog2e = 1.4426950408889634f;
 // The reference of the exponentials follows the running maximum only when that has moved more than 2^kRescaleStep above it.
 constexpr float kRescaleStep = 8.f;
+constexpr float kLn2 = 0.6931471805599453f;
+constexpr float kNoScore = -3e38f;  // a reference below all scores, and finite: scores of -inf give weights of zero against it
 
 struct PromptArgs {
   const void* q;
@@ -70,7 +71,7 @@ struct Item {
 
 // Prompts' row tiles: tiles_b = ceil(len_b G / rows).  Up to 64 prompts: level by level from the longest prompt's last tile
 // down, so that no long tile is dispatched after short ones.  C(L) = sum_b max(0, tiles_b - L) tiles lie at level L and above.
-template <int kRows>
+template <int kRows, int kThreads>
 __device__ inline Item find_item(const PromptArgs& a, int rank) {
   const int lane = threadIdx.x & (kWave - 1);
   __shared__ int64_t s_sum[kThreads];
@@ -140,16 +141,17 @@ __device__ inline Item find_item(const PromptArgs& a, int rank) {
 }
 
 // ---- staging: global memory -> registers -> LDS, in 16-byte chunks of rows ----------------------------------------------
-// Chunk c of row `key` lies at position c ^ swizzle(key): 16 consecutive rows put the same chunk at 16 positions of a 256-byte
-// line (the score product reads a row per lane), and the output product's reads are free of bank conflicts too.
+// Chunk c of row `key` lies at position c ^ swizzle(key), so that the reads of both products (a row per lane; four rows of
+// sixteen elements per sixteen lanes) are free of bank conflicts.  (Bit 2 of the key takes no part: rows four apart are read by
+// the same lanes, at a constant distance.)
 template <typename T, int D>
 __device__ inline int swizzle(int key) {
   if (sizeof(T) == 4) return (key & 7) | ((((key >> 2) ^ (key >> 3)) & 1) << 3);
-  if (D == 128) return ((key & 7) << 1) | ((key >> 3) & 1);
-  return (((key >> 1) & 3) << 1) | ((key >> 3) & 1);
+  if (D == 128) return ((key & 3) << 1) | ((key >> 3) & 1);
+  return (key & 2) | ((key >> 3) & 1);
 }
 
-template <typename T, int D>
+template <typename T, int D, int kThreads>
 struct Stage {
   static constexpr int kE = 16 / (int)sizeof(T);
   static constexpr int kRowChunks = D / kE;
@@ -178,105 +180,34 @@ struct Stage {
 };
 
 // ---- the two products of a wavefront's rows with 32 staged keys ----------------------------------------------------------
-template <typename T, int D> struct Products;
-
 template <int D>
-struct Products<__bf16, D> {
-  typedef bf16x8 Query[D / 16];
-  static constexpr int kRowChunks = D / 8;
-  __device__ static void load_query(Query& q, const __bf16* row, int h) {
-#pragma unroll
-    for (int ks = 0; ks < D / 16; ++ks) q[ks] = *(const bf16x8*)(row + 16 * ks + 8 * h);
-  }
-  template <int R>
-  __device__ static void scores(floatx16 (&s)[R], const uintx4* kt, const Query (&q)[R], int lane) {
-    const int h = lane >> 5, j = lane & 31;
-#pragma unroll
-    for (int r = 0; r < R; ++r) s[r] = (floatx16)(0.f);
-    bf16x8 kx[D / 16];
-#pragma unroll
-    for (int ks = 0; ks < D / 16; ++ks)
-      kx[ks] = __builtin_bit_cast(bf16x8, kt[j * kRowChunks + ((2 * ks + h) ^ swizzle<__bf16, D>(j))]);
-#pragma unroll
-    for (int ks = 0; ks < D / 16; ++ks)
-#pragma unroll
-      for (int r = 0; r < R; ++r) s[r] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kx[ks], q[r][ks], s[r], 0, 0, 0);
-  }
-  // p[r]: the probabilities; rounded[r] becomes the sum of those that enter the product (this lane's).
-  template <int R>
-  __device__ static void output(floatx16 (&o)[R][D / 32], const uintx4* vt, const floatx16 (&p)[R], float (&rounded)[R], int lane) {
-    const int h = lane >> 5, li = lane & 15, jh = (lane >> 4) & 1;
-#pragma unroll
-    for (int r = 0; r < R; ++r) rounded[r] = 0.f;
-#pragma unroll
-    for (int kk = 0; kk < 2; ++kk) {
-      bf16x8 pb[R];
-#pragma unroll
-      for (int r = 0; r < R; ++r) {
-        floatx8 x;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = p[r][8 * kk + e];
-        pb[r] = __builtin_convertvector(x, bf16x8);
-        const floatx8 y = __builtin_convertvector(pb[r], floatx8);
-        rounded[r] += ((y[0] + y[1]) + (y[2] + y[3])) + ((y[4] + y[5]) + (y[6] + y[7]));
-      }
-#pragma unroll
-      for (int jt = 0; jt < D / 32; ++jt) {
-        // transposing reads: sixteen lanes fetch four rows of sixteen elements, lane i receives column i
-        shortx4 part[2];
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          const int token = 16 * kk + 8 * half + 4 * h + (li >> 2), chunk = 4 * jt + 2 * jh + ((li & 3) >> 1);
-          const char* at = (const char*)(vt + token * kRowChunks + (chunk ^ swizzle<__bf16, D>(token))) + 8 * (li & 1);
-          part[half] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4*)at);
-        }
-        const bf16x8 v = __builtin_bit_cast(bf16x8, __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7));
-#pragma unroll
-        for (int r = 0; r < R; ++r) o[r][jt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, pb[r], o[r][jt], 0, 0, 0);
-      }
-    }
-  }
-};
-
-template <int D>
-struct Products<float, D> {
+struct ProductsF32 {
   typedef floatx4 Query[D / 8];
   static constexpr int kRowChunks = D / 4;
   __device__ static void load_query(Query& q, const float* row, int h) {
 #pragma unroll
     for (int s = 0; s < D / 8; ++s) q[s] = *(const floatx4*)(row + 8 * s + 4 * h);
   }
-  template <int R>
-  __device__ static void scores(floatx16 (&s)[R], const uintx4* kt, const Query (&q)[R], int lane) {
+  __device__ static floatx16 scores(const uintx4* kt, const Query& q, int lane) {
     const int h = lane >> 5, j = lane & 31;
-#pragma unroll
-    for (int r = 0; r < R; ++r) s[r] = (floatx16)(0.f);
+    floatx16 s = (floatx16)(0.f);
 #pragma unroll
     for (int x = 0; x < D / 8; ++x) {  // contraction step (x, e): the halves hold head dims 8 x + e and 8 x + 4 + e
       const floatx4 k = __builtin_bit_cast(floatx4, kt[j * kRowChunks + ((2 * x + h) ^ swizzle<float, D>(j))]);
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-#pragma unroll
-        for (int r = 0; r < R; ++r) s[r] = __builtin_amdgcn_mfma_f32_32x32x2f32(k[e], q[r][x][e], s[r], 0, 0, 0);
+      for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_32x32x2f32(k[e], q[x][e], s, 0, 0, 0);
     }
+    return s;
   }
-  template <int R>
-  __device__ static void output(floatx16 (&o)[R][D / 32], const uintx4* vt, const floatx16 (&p)[R], float (&rounded)[R], int lane) {
+  __device__ static void output(floatx16 (&o)[D / 32], const uintx4* vt, const floatx16& p, int lane) {
     const int h = lane >> 5, j = lane & 31;
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-      rounded[r] = 0.f;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) rounded[r] += p[r][i];
-    }
 #pragma unroll
     for (int i = 0; i < 16; ++i) {  // register i of the halves: two keys
       const int key = key_of(i, h);
 #pragma unroll
       for (int jt = 0; jt < D / 32; ++jt) {
         const float v = ((const float*)(vt + key * kRowChunks + ((8 * jt + (j >> 2)) ^ swizzle<float, D>(key))))[j & 3];
-#pragma unroll
-        for (int r = 0; r < R; ++r) o[r][jt] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, p[r][i], o[r][jt], 0, 0, 0);
+        o[jt] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, p[i], o[jt], 0, 0, 0);
       }
     }
   }
@@ -284,8 +215,6 @@ struct Products<float, D> {
 
 __device__ inline float widen(float x) { return x; }
 __device__ inline float widen(__bf16 x) { return (float)x; }
-__device__ inline void store4(float* p, floatx4 x) { *(floatx4*)p = x; }
-__device__ inline void store4(__bf16* p, floatx4 x) { *(bf16x4*)p = __builtin_convertvector(x, bf16x4); }
 
 // One row again, key by key, by the whole wavefront: for rows that are hardly ever seen, small and not fast.
 template <typename T, int D>
@@ -316,40 +245,35 @@ __device__ void walk(const PromptArgs& a, int base, int token, int head, int lan
   for (int i = 0; i < K; ++i) out[lane + i * kWave] = (T)(acc[i] * inv);
 }
 
-template <typename T, int D, int R>
-__global__ __launch_bounds__(kThreads, 1) void prompt_attention_kernel(PromptArgs a) {
-  constexpr int kRows = kWaves * kTile * R;
-  typedef Products<T, D> P;
-  typedef Stage<T, D> S;
+// ---- fp32 -----------------------------------------------------------------------------------------------------------------
+template <int D>
+__global__ __launch_bounds__(256, 1) void prompt_f32_kernel(PromptArgs a) {
+  constexpr int kThreads = 256, kRows = kThreads / kWave * kTile;
+  typedef ProductsF32<D> P;
+  typedef Stage<float, D, kThreads> S;
   __shared__ uintx4 lds[2][2 * S::kChunks];
   const int tid = threadIdx.x, lane = tid & (kWave - 1), h = lane >> 5, j = lane & 31;
   const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
-  // consecutive workgroups go to different L2s: the row tiles of one kv head sit behind as few of them as possible
   const int g = blockIdx.x % a.Hkv, rank = blockIdx.x / a.Hkv;
-  const Item it = find_item<kRows>(a, rank);
+  const Item it = find_item<kRows, kThreads>(a, rank);
   if (it.tile < 0 || it.len <= 0) return;
   const int base = __builtin_amdgcn_readfirstlane(it.base), len = __builtin_amdgcn_readfirstlane(it.len);
   const int rows = len * a.G, row0 = __builtin_amdgcn_readfirstlane(it.tile) * kRows;
-  const int mine = row0 + wv * kTile * R;  // this wavefront's first row
+  const int mine = row0 + wv * kTile;                        // this wavefront's first row
   const int keys = (min(row0 + kRows, rows) - 1) / a.G + 1;  // keys of the workgroup
-  const int last = (min(mine + kTile * R, rows) - 1) / a.G;  // the last key of the wavefront (with rows)
+  const int last = (min(mine + kTile, rows) - 1) / a.G;      // the last key of the wavefront (with rows)
+  const int first = min(mine, rows - 1) / a.G;               // and its first token
 
-  typename P::Query q[R];
-  floatx16 o[R][D / 32];
-  float m[R], l[R], exact[R];
-  int token[R];
+  const int rho = min(mine + j, rows - 1);  // padding rows repeat the last real row; never written
+  const int token = rho / a.G, head = g * a.G + rho % a.G;
+  typename P::Query q;
+  P::load_query(q, (const float*)a.q + (int64_t)(base + token) * a.q_stride + (int64_t)head * D, h);
+  floatx16 o[D / 32];
 #pragma unroll
-  for (int r = 0; r < R; ++r) {
-    const int rho = min(mine + kTile * r + j, rows - 1);  // padding rows repeat the last real row; never written
-    token[r] = rho / a.G;
-    P::load_query(q[r], (const T*)a.q + (int64_t)(base + token[r]) * a.q_stride + (int64_t)(g * a.G + rho % a.G) * D, h);
-#pragma unroll
-    for (int jt = 0; jt < D / 32; ++jt) o[r][jt] = (floatx16)(0.f);
-    m[r] = -INFINITY;
-    l[r] = exact[r] = 0.f;
-  }
-  const T* kp = (const T*)a.k + (int64_t)base * a.k_stride + (int64_t)g * D;
-  const T* vp = (const T*)a.v + (int64_t)base * a.v_stride + (int64_t)g * D;
+  for (int jt = 0; jt < D / 32; ++jt) o[jt] = (floatx16)(0.f);
+  float m = -INFINITY, l = 0.f;
+  const float* kp = (const float*)a.k + (int64_t)base * a.k_stride + (int64_t)g * D;
+  const float* vp = (const float*)a.v + (int64_t)base * a.v_stride + (int64_t)g * D;
   const int steps = (keys + S::kKeys - 1) / S::kKeys;
   S stage;
   stage.load(kp, vp, a, 0, len, tid);
@@ -358,90 +282,375 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_attention_kernel(PromptArg
     stage.store(at, tid);
     if (t + 1 < steps) stage.load(kp, vp, a, (t + 1) * S::kKeys, len, tid);
     __syncthreads();  // the stage is full, and everyone is done with the other one
-    if (mine >= rows) continue;
-    for (int x = 0; x < S::kKeys; x += kTile) {
-      const int key0 = t * S::kKeys + x;
-      if (key0 > last) break;
-      floatx16 s[R];
-      P::scores(s, at + x * S::kRowChunks, q, lane);
-      float rounded[R];
+    const int key0 = t * S::kKeys;
+    if (mine >= rows || key0 > last) continue;
+    floatx16 s = P::scores(at, q, lane);
+    if (key0 + kTile - 1 > first) {
 #pragma unroll
-      for (int r = 0; r < R; ++r) {
-        const int first = (min(mine + kTile * r, rows - 1)) / a.G;  // the row tile's first token
-        if (key0 + kTile - 1 > first) {
-#pragma unroll
-          for (int i = 0; i < 16; ++i)
-            if (key0 + key_of(i, h) > token[r]) s[r][i] = -INFINITY;
-        }
-        float mx = s[r][0];
-#pragma unroll
-        for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[r][i]);
-        const float m_new = fmaxf(m[r], max_halves(mx));
-        if (__any((m_new - m[r]) * a.c > kRescaleStep)) {
-          const float alpha = __builtin_amdgcn_exp2f((m[r] - (m_new == -INFINITY ? 0.f : m_new)) * a.c);
-          l[r] *= alpha;
-          exact[r] *= alpha;
-#pragma unroll
-          for (int jt = 0; jt < D / 32; ++jt) o[r][jt] *= alpha;
-          m[r] = m_new;
-        }
-        const float mc = m[r] == -INFINITY ? 0.f : m[r] * a.c;
-        float sum = 0.f;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          s[r][i] = __builtin_amdgcn_exp2f(fmaf(s[r][i], a.c, -mc));
-          sum += s[r][i];
-        }
-        exact[r] += sum;
-      }
-      P::output(o, at + S::kChunks + x * S::kRowChunks, s, rounded, lane);
-#pragma unroll
-      for (int r = 0; r < R; ++r) l[r] += rounded[r];
+      for (int i = 0; i < 16; ++i)
+        if (key0 + key_of(i, h) > token) s[i] = -INFINITY;
     }
+    float mx = s[0];
+#pragma unroll
+    for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[i]);
+    const float m_new = fmaxf(m, max_halves(mx));
+    if (__any((m_new - m) * a.c > kRescaleStep)) {
+      const float alpha = __builtin_amdgcn_exp2f((m - (m_new == -INFINITY ? 0.f : m_new)) * a.c);
+      l *= alpha;
+#pragma unroll
+      for (int jt = 0; jt < D / 32; ++jt) o[jt] *= alpha;
+      m = m_new;
+    }
+    const float mc = m == -INFINITY ? 0.f : m * a.c;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], a.c, -mc));
+      l += s[i];
+    }
+    P::output(o, at + S::kChunks, s, lane);
   }
   if (mine >= rows) return;
+  const bool there = mine + j < rows;
+  const float sum = sum_halves(l), inv = sum > 0.f ? 1.f / sum : 0.f;
+  float bad = 0.f;
 #pragma unroll
-  for (int r = 0; r < R; ++r) {
-    const int rho = mine + kTile * r + j;
-    const bool there = rho < rows;
-    const float sum = sum_halves(l[r]), inv = sum > 0.f ? 1.f / sum : 0.f;
-    const float all = sum_halves(exact[r]);
-    const int head = g * a.G + (there ? rho : rows - 1) % a.G;
-    float bad = 0.f;
+  for (int jt = 0; jt < D / 32; ++jt)
 #pragma unroll
-    for (int jt = 0; jt < D / 32; ++jt)
+    for (int i4 = 0; i4 < 4; ++i4) {
+      floatx4 x;
 #pragma unroll
-      for (int i4 = 0; i4 < 4; ++i4) {
-        floatx4 x;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          x[i] = o[r][jt][4 * i4 + i] * inv;
-          bad = fmaf(x[i], 0.f, bad);
-        }
-        if (there) store4((T*)a.out + (int64_t)(base + token[r]) * a.out_stride + (int64_t)head * D + 32 * jt + 8 * i4 + 4 * h, x);
+      for (int i = 0; i < 4; ++i) {
+        x[i] = o[jt][4 * i4 + i] * inv;
+        bad = fmaf(x[i], 0.f, bad);
       }
-    if (a.lse && there && h == 0) a.lse[(int64_t)(base + token[r]) * a.Hq + head] = all > 0.f ? m[r] * a.scale + logf(all) : -INFINITY;
-    // an infinity or NaN that does not come from NaN scores (those stay NaN whichever way they are summed)
-    uint64_t again = __ballot(there && bad != 0.f && sum < INFINITY);
-    again = (again | again >> 32) & 0xFFFFFFFFull;
-    while (again) {
-      const int i = __ffsll((unsigned long long)again) - 1;
-      again &= again - 1;
-      const int row = mine + kTile * r + i;
-      walk<T, D>(a, base, row / a.G, g * a.G + row % a.G, lane);
+      if (there) *(floatx4*)((float*)a.out + (int64_t)(base + token) * a.out_stride + (int64_t)head * D + 32 * jt + 8 * i4 + 4 * h) = x;
     }
+  if (a.lse && there && h == 0) a.lse[(int64_t)(base + token) * a.Hq + head] = sum > 0.f ? m * a.scale + logf(sum) : -INFINITY;
+  uint64_t again = __ballot(there && bad != 0.f && sum < INFINITY);
+  again = (again | again >> 32) & 0xFFFFFFFFull;
+  for (; again; again &= again - 1) {
+    const int row = mine + __ffsll((unsigned long long)again) - 1;
+    walk<float, D>(a, base, row / a.G, g * a.G + row % a.G, lane);
   }
 }
 
-template <typename T, int D, int R>
-int32_t launch(const PromptArgs& a, hipStream_t stream) {
-  constexpr int kRows = kWaves * kTile * R;
-  const int64_t tiles = (int64_t)a.total_tokens * a.G / kRows + a.batch;  // sum of ceil(len G / rows) is at most that
-  const int64_t grid = tiles * a.Hkv;
+// ---- bf16 -----------------------------------------------------------------------------------------------------------------
+// Two bf16 ones: the sum of a pair of rounded probabilities is one dot product.
+__device__ inline float add_pair(uint32_t pair, float sum) {
+  return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pair), __builtin_bit_cast(bf16x2, 0x3F803F80u), sum, false);
+}
+__device__ inline float max_quarters(float x) {  // over the lanes with the same lane % 16
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return max_halves(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
+}
+__device__ inline float sum_quarters(float x) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return sum_halves(__uint_as_float(r[0]) + __uint_as_float(r[1]));
+}
+
+__device__ inline float highest(const floatx8& x) {
+  return fmaxf(fmaxf(fmaxf(fmaxf(x[0], x[1]), x[2]), fmaxf(x[3], x[4])), fmaxf(fmaxf(x[5], x[6]), x[7]));
+}
+
+typedef __attribute__((address_space(3))) char lds_char;
+typedef __attribute__((address_space(3))) uintx4 lds_uintx4;
+
+// A wavefront's 16 N rows: products of 16 x 16 tiles, 32 keys at a time.  Lane (quarter w, i): of a score tile, row i and four
+// keys; the two score tiles of a step are made of keys 8 w + 0 .. 3 and 8 w + 4 .. 7, so that a lane's eight probabilities are
+// the eight consecutive keys that it contributes to the output product.
+template <int D, int N, bool kLse>
+struct RowsBf16 {
+  bf16x8 q[N][D / 32];
+  floatx4 o[N][D / 16];
+  float mc[N], l[N], exact[N];  // the reference (in powers of two); the sums of the rounded weights and of the unrounded ones
+  int token[N];
+  uint32_t ka[D / 32], va[D / 16];  // byte offsets in a stage of this lane's vectors
+
+  __device__ void begin(const PromptArgs& a, int base, int g, int mine, int rows, int lane, int value_offset) {
+    const int w = lane >> 4, i = lane & 15;
+#pragma unroll
+    for (int r = 0; r < N; ++r) {
+      const int rho = min(mine + 16 * r + i, rows - 1);  // padding rows repeat the last real row; never written
+      token[r] = rho / a.G;
+      const __bf16* qp = (const __bf16*)a.q + (int64_t)(base + token[r]) * a.q_stride + (int64_t)(g * a.G + rho % a.G) * D + 8 * w;
+#pragma unroll
+      for (int ks = 0; ks < D / 32; ++ks) q[r][ks] = *(const bf16x8*)(qp + 32 * ks);
+#pragma unroll
+      for (int dt = 0; dt < D / 16; ++dt) o[r][dt] = (floatx4)(0.f);
+      mc[r] = kNoScore;
+      l[r] = exact[r] = 0.f;
+    }
+    const int k_key = 8 * (i >> 2) + (i & 3), v_key = 8 * w + (i >> 2);
+#pragma unroll
+    for (int ks = 0; ks < D / 32; ++ks) ka[ks] = k_key * (2 * D) + ((4 * ks + w) ^ swizzle<__bf16, D>(k_key)) * 16;
+#pragma unroll
+    for (int dt = 0; dt < D / 16; ++dt)
+      va[dt] = value_offset + v_key * (2 * D) + ((2 * dt + ((i & 3) >> 1)) ^ swizzle<__bf16, D>(v_key)) * 16 + 8 * (i & 1);
+  }
+  // The operands of the products with keys 32 x .. of the stage at `at`.
+  __device__ void read_keys(bf16x8 (&k)[D / 32][2], lds_char* at, int x) const {
+#pragma unroll
+    for (int ks = 0; ks < D / 32; ++ks)
+#pragma unroll
+      for (int half = 0; half < 2; ++half)
+        k[ks][half] = __builtin_bit_cast(bf16x8, *(lds_uintx4*)(at + ka[ks] + (32 * x + 4 * half) * (2 * D)));
+  }
+  __device__ void read_values(bf16x8 (&v)[D / 16], lds_char* at, int x) const {
+    // transposing reads: sixteen lanes fetch four rows of sixteen elements, lane i receives column i
+#pragma unroll
+    for (int dt = 0; dt < D / 16; ++dt) {
+      shortx4 four[2];
+#pragma unroll
+      for (int half = 0; half < 2; ++half)
+        four[half] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4*)(at + va[dt] + (32 * x + 4 * half) * (2 * D)));
+      v[dt] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(four[0], four[1], 0, 1, 2, 3, 4, 5, 6, 7));
+    }
+  }
+  __device__ void scores(floatx4 (&s)[N][2], const bf16x8 (&k)[D / 32][2]) const {
+#pragma unroll
+    for (int ks = 0; ks < D / 32; ++ks)
+#pragma unroll
+      for (int half = 0; half < 2; ++half)
+#pragma unroll
+        for (int r = 0; r < N; ++r)
+          s[r][half] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[ks][half], q[r][ks], ks == 0 ? (floatx4)(0.f) : s[r][half], 0, 0, 0);
+  }
+  __device__ void mask(floatx4 (&s)[N][2], int key0, int lane) const {
+#pragma unroll
+    for (int r = 0; r < N; ++r)
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (e > token[r] - key0 - 8 * (lane >> 4)) s[r][e >> 2][e & 3] = -INFINITY;
+  }
+  // Scores -> probabilities as the output product takes them.  The values are requested between the exponentials: a wavefront
+  // that asks for all of them at once waits until the LDS has taken the requests of all wavefronts.
+  __device__ void softmax(bf16x8 (&pb)[N], const floatx4 (&s)[N][2], float c, bf16x8 (&v)[D / 16], lds_char* at, int part) {
+    floatx8 e2[N];
+    if (__any(exponents(e2, s, c))) rescale(e2, s, c);
+    __builtin_amdgcn_sched_barrier(0);
+    read_values(v, at, part);
+    weights(pb, e2);
+#pragma unroll
+    for (int i = 0; i < D / 8; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x2, N + (kLse ? 1 : 0), 0);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  // The reference of the exponentials stays while no score is more than 2^kRescaleStep above it; a lane looks at its own scores only,
+  // and where one is (true), the rows' maxima are taken.
+  __device__ bool exponents(floatx8 (&e2)[N], const floatx4 (&s)[N][2], float c) const {
+    bool move = false;
+#pragma unroll
+    for (int r = 0; r < N; ++r) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) e2[r][e] = fmaf(s[r][e >> 2][e & 3], c, -mc[r]);
+      move = move || highest(e2[r]) > kRescaleStep;
+    }
+    return move;
+  }
+  __device__ void rescale(floatx8 (&e2)[N], const floatx4 (&s)[N][2], float c) {
+#pragma unroll
+    for (int r = 0; r < N; ++r) {
+      floatx8 raw;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) raw[e] = s[r][e >> 2][e & 3];
+      const float now = fmaxf(mc[r], max_quarters(highest(raw)) * c), alpha = __builtin_amdgcn_exp2f(mc[r] - now);
+      l[r] *= alpha;
+      exact[r] *= alpha;
+#pragma unroll
+      for (int dt = 0; dt < D / 16; ++dt) o[r][dt] *= alpha;
+      mc[r] = now;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) e2[r][e] = fmaf(raw[e], c, -now);
+    }
+  }
+  __device__ void weights(bf16x8 (&pb)[N], const floatx8 (&e2)[N]) {
+#pragma unroll
+    for (int r = 0; r < N; ++r) {
+      floatx8 p;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) p[e] = __builtin_amdgcn_exp2f(e2[r][e]);
+      if (kLse) exact[r] += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
+      pb[r] = __builtin_convertvector(p, bf16x8);
+      const uintx4 pairs = __builtin_bit_cast(uintx4, pb[r]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) l[r] = add_pair(pairs[e], l[r]);
+    }
+  }
+  // The output product, while the keys 32 x .. of the stage at `at` are fetched.
+  __device__ void output(const bf16x8 (&v)[D / 16], const bf16x8 (&pb)[N], bf16x8 (&k)[D / 32][2], lds_char* at, int part) {
+    read_keys(k, at, part);
+#pragma unroll
+    for (int dt = 0; dt < D / 16; ++dt)
+#pragma unroll
+      for (int r = 0; r < N; ++r) o[r][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[dt], pb[r], o[r][dt], 0, 0, 0);
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x8, N, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  __device__ void finish(const PromptArgs& a, int base, int g, int mine, int rows, int lane) {
+    const int w = lane >> 4, i = lane & 15;
+#pragma unroll
+    for (int r = 0; r < N; ++r) {
+      const int rho = mine + 16 * r + i;
+      const bool there = rho < rows;
+      const float sum = sum_quarters(l[r]), inv = sum > 0.f ? 1.f / sum : 0.f;
+      const int head = g * a.G + (there ? rho : rows - 1) % a.G;
+      __bf16* out = (__bf16*)a.out + (int64_t)(base + token[r]) * a.out_stride + (int64_t)head * D + 4 * w;
+      float bad = 0.f;
+#pragma unroll
+      for (int dt = 0; dt < D / 16; ++dt) {
+        const floatx4 x = o[r][dt] * inv;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) bad = fmaf(x[e], 0.f, bad);
+        if (there) *(bf16x4*)(out + 16 * dt) = __builtin_convertvector(x, bf16x4);
+      }
+      if (kLse) {
+        const float all = sum_quarters(exact[r]);
+        if (there && w == 0) a.lse[(int64_t)(base + token[r]) * a.Hq + head] = all > 0.f ? mc[r] * kLn2 + logf(all) : -INFINITY;
+      }
+      // an infinity or NaN that does not come from NaN scores (those stay NaN whichever way they are summed)
+      uint64_t again = __ballot(there && bad != 0.f && sum < INFINITY);
+      again |= again >> 32;
+      again = (again | again >> 16) & 0xFFFFull;
+      for (; again; again &= again - 1) {
+        const int row = mine + 16 * r + __ffsll((unsigned long long)again) - 1;
+        walk<__bf16, D>(a, base, row / a.G, g * a.G + row % a.G, lane);
+      }
+    }
+  }
+};
+
+// A stage is 64 keys, two parts of 32.  Stage t lies in buffer t % 2.  It is written behind the barrier of stage t - 2, when nobody
+// reads that one any more, out of registers that were requested a stage earlier, and first read (the keys of its first part)
+// behind the barrier of stage t - 1.
+template <int D, int kWaves, int N, bool kLse>
+__global__ __launch_bounds__(kWaves* kWave, 2) void prompt_bf16_kernel(PromptArgs a) {
+  constexpr int kThreads = kWaves * kWave, kMine = 16 * N, kRows = kWaves * kMine;
+  typedef Stage<__bf16, D, kThreads> S;
+  static_assert(S::kKeys == 64, "two parts a stage");
+  __shared__ uintx4 lds[2][2 * S::kChunks];
+  const int tid = threadIdx.x, lane = tid & (kWave - 1);
+  const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
+  // consecutive workgroups go to different L2s: the row tiles of one kv head sit behind as few of them as possible
+  const int g = blockIdx.x % a.Hkv, rank = blockIdx.x / a.Hkv;
+  const Item it = find_item<kRows, kThreads>(a, rank);
+  if (it.tile < 0 || it.len <= 0) return;
+  const int base = __builtin_amdgcn_readfirstlane(it.base), len = __builtin_amdgcn_readfirstlane(it.len);
+  const int rows = len * a.G, row0 = __builtin_amdgcn_readfirstlane(it.tile) * kRows;
+  const int mine = row0 + wv * kMine;                                       // this wavefront's first row
+  const int keys = (min(row0 + kRows, rows) - 1) / a.G + 1;                 // keys of the workgroup
+  const int last = mine < rows ? (min(mine + kMine, rows) - 1) / a.G : -1;  // the last key of the wavefront
+  const int first = min(mine, rows - 1) / a.G;                              // its first token
+  const int steps = (keys + S::kKeys - 1) / S::kKeys;
+
+  const __bf16* kp = (const __bf16*)a.k + (int64_t)base * a.k_stride + (int64_t)g * D;
+  const __bf16* vp = (const __bf16*)a.v + (int64_t)base * a.v_stride + (int64_t)g * D;
+  S stage;
+  stage.load(kp, vp, a, 0, len, tid);
+  RowsBf16<D, N, kLse> x;
+  x.begin(a, base, g, mine, rows, lane, S::kChunks * 16);
+  stage.store(lds[0], tid);
+  if (steps > 1) {
+    stage.load(kp, vp, a, S::kKeys, len, tid);
+    stage.store(lds[1], tid);
+    if (steps > 2) stage.load(kp, vp, a, 2 * S::kKeys, len, tid);
+  }
+  __syncthreads();
+
+  lds_char* at = (lds_char*)lds[0];
+  lds_char* other = (lds_char*)lds[1];
+  int t = 0;
+  auto fill = [&]() {  // behind the barrier of stage t
+    if (t + 2 < steps) {
+      stage.store(lds[t & 1], tid);
+      if (t + 3 < steps) stage.load(kp, vp, a, (t + 3) * S::kKeys, len, tid);
+    }
+  };
+  auto next_stage = [&]() {
+    lds_char* const was = at;
+    at = other;
+    other = was;
+    ++t;
+  };
+  bf16x8 k[D / 32][2], v[D / 16], pb[N];
+  floatx4 s[N][2];
+  x.read_keys(k, at, 0);
+  x.scores(s, k);
+  // Stages that all rows of the wavefront see whole.
+  const int whole = mine < rows ? (first + 1) / S::kKeys : 0;
+  while (t < whole) {
+#pragma unroll
+    for (int part = 0; part < 2; ++part) {
+      x.softmax(pb, s, a.c, v, at, part);
+      if (part == 1) {
+        __syncthreads();
+        fill();
+      }
+      __builtin_amdgcn_s_setprio(1);
+      x.output(v, pb, k, part == 0 ? at : other, 1 - part);  // (behind the last stage of no use, but there to be read)
+      x.scores(s, k);
+      __builtin_amdgcn_s_setprio(0);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    next_stage();
+  }
+  // the diagonal and the prompt's end; wavefronts that are done keep the stages coming
+  while (t < steps) {
+#pragma unroll
+    for (int part = 0; part < 2; ++part) {
+      const int key0 = t * S::kKeys + 32 * part;
+      if (key0 <= last) {
+        x.mask(s, key0, lane);
+        x.softmax(pb, s, a.c, v, at, part);
+      }
+      if (part == 1) {
+        __syncthreads();
+        fill();
+      }
+      if (key0 <= last) {
+        x.output(v, pb, k, part == 0 ? at : other, 1 - part);
+        x.scores(s, k);
+      }
+    }
+    next_stage();
+  }
+  if (mine < rows) x.finish(a, base, g, mine, rows, lane);
+}
+
+// Row tiles of the given height that any offsets can make: sum of ceil(len G / rows) is at most that.
+int64_t most_tiles(const PromptArgs& a, int rows) { return (int64_t)a.total_tokens * a.G / rows + a.batch; }
+
+template <typename Kernel>
+int32_t launch(Kernel kernel, int threads, int rows, const PromptArgs& a, hipStream_t stream) {
+  const int64_t grid = most_tiles(a, rows) * a.Hkv;
   if (grid > 0x7FFFFFFF) return SMART_EINVAL;
-  hipLaunchKernelGGL((prompt_attention_kernel<T, D, R>), dim3((unsigned)grid), dim3(kThreads), 0, stream, a);
+  hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(threads), 0, stream, a);
   SMART_HIP_CHECK(hipGetLastError());
   return SMART_OK;
+}
+
+template <int D, int kWaves, int N>
+int32_t launch_rows(const PromptArgs& a, hipStream_t stream) {
+  return a.lse ? launch(prompt_bf16_kernel<D, kWaves, N, true>, kWaves * kWave, kWaves * 16 * N, a, stream)
+               : launch(prompt_bf16_kernel<D, kWaves, N, false>, kWaves * kWave, kWaves * 16 * N, a, stream);
+}
+
+// Taller row tiles read the LDS less often per product, but there have to be enough of them to fill the chip and to let the short
+// ones fill in behind the long.  us with tiles of 64 / 128 / 256 rows (four wavefronts; 256 rows of head dim 128 eight), 32 / 8
+// heads: one prompt of 37 tokens 5.3 / 6.3 / 6.9, of 512 14.4 / 18.6 / 23; 4 of 512 26.7 / 22.3 / 26; one of 2048 70 / 59 / 64; 8262
+// tokens 256 / 172.9 / 171.8; 16384 tokens, 64 heads 6633 / 4307 / 3831; head dim 64, 64 prompts of 1 .. 300 tokens, 8 heads 14.1 /
+// 12.1 / 14.8, 4 of 4096 420 / 325 / 301.
+template <int D>
+int32_t launch_bf16(const smart_ctx* ctx, const PromptArgs& a, hipStream_t stream) {
+  const int64_t rows = (int64_t)a.total_tokens * a.Hq, cus = ctx->num_cus > 0 ? ctx->num_cus : 256;
+  if (rows <= 128 * cus) return launch_rows<D, 4, 1>(a, stream);
+  if (rows < 4 * 256 * cus) return launch_rows<D, 4, 2>(a, stream);
+  return launch_rows<D, D == 128 ? 8 : 4, D == 128 ? 2 : 4>(a, stream);
 }
 
 int32_t check(const prompt_params& p) {
@@ -489,8 +698,11 @@ extern "C" int32_t prompt_attention(smart_ctx* ctx, void* stream, const prompt_p
   SMART_HIP_CHECK(hipGetDevice(&prev));
   if (prev != ctx->device) SMART_HIP_CHECK(hipSetDevice(ctx->device));
   hipStream_t s = (hipStream_t)stream;
-  if (p.dtype == SMART_F32) rc = p.head_dim == 128 ? launch<float, 128, 1>(a, s) : launch<float, 64, 1>(a, s);
-  else rc = p.head_dim == 128 ? launch<__bf16, 128, 1>(a, s) : launch<__bf16, 64, 1>(a, s);
+  if (p.dtype == SMART_F32) {
+    rc = p.head_dim == 128 ? launch(prompt_f32_kernel<128>, 256, 128, a, s) : launch(prompt_f32_kernel<64>, 256, 128, a, s);
+  } else {
+    rc = p.head_dim == 128 ? launch_bf16<128>(ctx, a, s) : launch_bf16<64>(ctx, a, s);
+  }
   if (prev != ctx->device) (void)hipSetDevice(prev);
   return rc;
 }

@@ -74,6 +74,57 @@ def test_several_row_tiles(lib, dtype, D, lens):
     _check(out, lse, q, k, v, cu, D ** -0.5, dtype)
 
 
+@pytest.mark.parametrize("D,Hq,Hkv,lens", [(128, 28, 4, [1500, 2, 700]), (64, 32, 8, [1500, 2, 700]),
+                                           (128, 64, 8, [3000, 1, 0, 1200, 77]), (64, 64, 8, [3000, 1, 0, 1200, 77])])
+@pytest.mark.parametrize("lse", [False, True])
+def test_large_calls_by_some_of_their_rows(lib, D, Hq, Hkv, lens, lse):
+    """Calls of enough rows for the taller row tiles; the oracle on the first, last and random rows of every prompt."""
+    import torch
+    cu = np.concatenate([[0], np.cumsum(lens)]).astype(np.int32)
+    q, k, v = _inputs(int(cu[-1]), Hq, Hkv, D, "bf16", 31)
+    got = lib.prompt_attention(q, k, v, torch.from_numpy(cu).cuda(), D ** -0.5, want_lse=lse)
+    out, got_lse = (_f64(got[0]), _f64(got[1])) if lse else (_f64(got), None)
+    assert np.isfinite(out).all()
+    q, k, v = _f64(q), _f64(k), _f64(v)
+    rng = np.random.default_rng(0)
+    for lo, hi in zip(cu[:-1], cu[1:]):
+        if hi == lo:
+            continue
+        edge = [lo, hi - 1, min(lo + 31, hi - 1), min(lo + 32, hi - 1), min(lo + 63, hi - 1), min(lo + 64, hi - 1)]
+        for t in set(edge) | set(rng.integers(lo, hi, 60).tolist()):
+            for h in {0, Hq - 1, int(rng.integers(Hq))}:
+                g = h // (Hq // Hkv)
+                ref, ref_lse, A, S = P.prompt_row(q[t, h], k[lo:t + 1, g], v[lo:t + 1, g], D ** -0.5)
+                u = (2 * D * S + 2 * (t + 1 - lo) + 16) * U
+                assert (np.abs(out[t, h] - ref) <= u * A + 2 * 2.0 ** -8 * A + 2.0 ** -8 * np.abs(ref)).all(), (t, h)
+                assert got_lse is None or abs(got_lse[t, h] - ref_lse) <= u + 2 * U * abs(ref_lse), (t, h)
+
+
+@pytest.mark.parametrize("first", [0, 5])
+def test_scores_of_minus_infinity_have_no_weight(lib, first):
+    """Keys whose products are -inf (bf16 holds it) count nothing, also where they come first; a row of nothing else is zero."""
+    import torch
+    for dtype in ("bf16", "f32"):
+        q, k, v = _inputs(90, 4, 2, 64, dtype, 17)
+        q[..., 0] = 1.0
+        k[first:first + 40, :, 0] = float("-inf")
+        cu = torch.tensor([0, 90], dtype=torch.int32, device="cuda")
+        out, lse = lib.prompt_attention(q, k, v, cu, 0.125, want_lse=True)
+        assert torch.isfinite(out).all()
+        keep = [t for t in range(90) if not first <= t < first + 40]
+        for t in (first + 3, first + 39, 70, 89):
+            own = [u for u in keep if u <= t]
+            for h in (0, 3):
+                if not own:
+                    assert (out[t, h] == 0).all() and lse[t, h] == float("-inf")
+                    continue
+                ref, ref_lse, A, S = P.prompt_row(_f64(q[t, h]), _f64(k[own, h // 2]), _f64(v[own, h // 2]), 0.125)
+                u = (2 * 64 * S + 2 * len(own) + 16) * U
+                tol = u * A + (2 * 2.0 ** -8 * A + 2.0 ** -8 * np.abs(ref) if dtype == "bf16" else U * np.abs(ref))
+                assert (np.abs(_f64(out[t, h]) - ref) <= tol).all()
+                assert abs(float(lse[t, h]) - ref_lse) <= u + 2 * U * abs(ref_lse)
+
+
 def test_many_prompts(lib):
     """More prompts than a wavefront has lanes; empty ones among them."""
     import torch
