@@ -98,6 +98,7 @@ struct TiledArgs {
   int32_t batch, total_nodes, Hq, Hkv, G, block_size, max_blocks, num_blocks;
   int32_t segment_cost;   // units of a segment beside its steps
   bool fp8, fp4, plain;   // the cache's element type and layout, where they are no template arguments
+  bool stream;            // the prefix kernel streams, and evaluates the trees of sequences with a prefix
   uint32_t block8_magic;  // token / 8 / (block_size / 8) by multiplication
   float scale;
   float c;         // softmax scale in powers of two (log2 e folded in)
@@ -252,6 +253,12 @@ __device__ inline int swizzle(int key) {
 }
 
 enum CacheType { kSameType, kE4M3, kE2M1 };
+
+// Whether the prefix kernel takes its operands straight from the pages (Fp4Stream).
+template <typename T>
+constexpr bool streams(CacheType cache, int D) {
+  return cache == kE2M1 && sizeof(T) == 2 && D == 128;
+}
 
 template <typename T, CacheType kCache, bool kPlain, int D>
 struct Stager {
@@ -751,7 +758,7 @@ struct Rows<float, kPlain, D> {
 };
 
 // ---- a 4-bit cache and few rows: operands straight from the pages -----------------------------------------------------------
-// One wavefront's 32 rows against tiles of 32 keys, head dim 128.  A lane's 16-byte vectors are its operands: of K, 32 head dims
+// One wavefront's 32 rows against tiles of 32 keys, head dim 128, and against the tree's nodes.  A lane's 16-byte vectors are its operands: of K, 32 head dims
 // of one key (the queries are laid out in the same order of the contraction); of V, four head dims of eight keys, a vector of
 // keys for each of the four output tiles (tile jt holds head dims 4 m + jt).  Nothing is shared between wavefronts, so nothing
 // goes through LDS and a wavefront keeps two tiles of its own in flight.
@@ -819,25 +826,8 @@ struct Fp4Stream {
       r.vs[kk] = *(const uint64_t*)(vp + (uint32_t)(id.vs[kk] * 8 + bs * (D / 2) + (d >> 5) * bs));
     }
   }
-  template <bool kMask>
-  __device__ void tile(Raw& r, int n_valid, float c, int lane) {
-    const int h = lane >> 5;
-    const uint32_t ks = r.ks >> (8 * h);
-    floatx16 s = (floatx16)(0.f);
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      const float sc = x == 0 ? smart::fp4_scale_of<0>(ks) : smart::fp4_scale_of<2>(ks);
-#pragma unroll
-      for (int w = 0; w < 4; ++w) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(bf16_of_codes(r.k[x][w], sc), q[4 * x + w], s, 0, 0, 0);
-    }
-    if (kMask && n_valid < 32) {
-      const int left = n_valid - 8 * h;  // register i: key 16 (i / 8) + 8 h + i % 8
-#pragma unroll
-      for (int i = 0; i < 16; ++i)
-        if (16 * (i >> 3) + (i & 7) >= left) s[i] = -INFINITY;
-#pragma unroll
-      for (int kk = 0; kk < 2; ++kk) keep_tokens(r.v[kk], r.vs[kk], left - 16 * kk);
-    }
+  // The reference, the sum and O follow the 32 scores; the probabilities of a lane's two times eight keys.
+  __device__ void softmax(bf16x8 (&pb)[2], const floatx16& s, float c) {
     float mx = s[0];
 #pragma unroll
     for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[i]);
@@ -857,17 +847,87 @@ struct Fp4Stream {
 #pragma unroll
       for (int e = 0; e < 8; ++e) p[e] = __builtin_amdgcn_exp2f(fmaf(s[8 * kk + e], c, -mc));
       l += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
-      const bf16x8 pb = __builtin_convertvector(p, bf16x8);
+      pb[kk] = __builtin_convertvector(p, bf16x8);
+    }
+  }
+  template <bool kMask>
+  __device__ void tile(Raw& r, int n_valid, float c, int lane) {
+    const int h = lane >> 5;
+    const uint32_t ks = r.ks >> (8 * h);
+    floatx16 s = (floatx16)(0.f);
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      const float sc = x == 0 ? smart::fp4_scale_of<0>(ks) : smart::fp4_scale_of<2>(ks);
+#pragma unroll
+      for (int w = 0; w < 4; ++w) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(bf16_of_codes(r.k[x][w], sc), q[4 * x + w], s, 0, 0, 0);
+    }
+    if (kMask && n_valid < 32) {
+      const int left = n_valid - 8 * h;  // register i: key 16 (i / 8) + 8 h + i % 8
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (16 * (i >> 3) + (i & 7) >= left) s[i] = -INFINITY;
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk) keep_tokens(r.v[kk], r.vs[kk], left - 16 * kk);
+    }
+    bf16x8 pb[2];
+    softmax(pb, s, c);
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk) {
       bf16x8 v[4];
       bf16_of_values(v, r.v[kk], r.vs[kk]);
 #pragma unroll
-      for (int jt = 0; jt < D / 32; ++jt) o[jt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[jt], pb, o[jt], 0, 0, 0);
+      for (int jt = 0; jt < D / 32; ++jt) o[jt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[jt], pb[kk], o[jt], 0, 0, 0);
     }
+  }
+  // Nodes 32 tt .. of a tree of n as 32 more keys, each seen by the rows of its descendants and its own.  (What a node that a row
+  // does not see holds is multiplied by zero: see row_overflowed.)
+  __device__ void tree_tile(const TiledArgs& a, int g, int base, int n, int row0, int rows, int tt, int lane) {
+    const int h = lane >> 5, j = lane & 31;
+    const int64_t stride = (int64_t)a.Hkv * D;
+    const __bf16* kt = (const __bf16*)a.k_tree + ((int64_t)base * a.Hkv + g) * D;
+    const __bf16* vt = (const __bf16*)a.v_tree + ((int64_t)base * a.Hkv + g) * D;
+    const int node = base + min(row0 + j, rows - 1) / a.G;
+    const uint64_t set = a.anc_mask[2 * (size_t)node + (tt >> 1)];
+    const int there = min(n - 32 * tt, 32);
+    const uint32_t seen = (uint32_t)(set >> (32 * (tt & 1))) & (there < 32 ? (1u << there) - 1u : ~0u);
+    const __bf16* kp = kt + min(32 * tt + (j & 16) + sigma(j & 15), n - 1) * stride + 32 * h;
+    bf16x8 kx[8];
+#pragma unroll
+    for (int c = 0; c < 2; ++c)
+#pragma unroll
+      for (int w = 0; w < 4; ++w) kx[4 * c + w] = *(const bf16x8*)(kp + 64 * c + 8 * w);
+    bf16x4 vx[2][8];
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) vx[kk][e] = *(const bf16x4*)(vt + min(32 * tt + 16 * kk + 8 * h + e, n - 1) * stride + 4 * j);
+    floatx16 s = (floatx16)(0.f);
+#pragma unroll
+    for (int x = 0; x < 8; ++x) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kx[x], q[x], s, 0, 0, 0);
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+      if (((seen >> (8 * h)) >> (16 * (i >> 3) + (i & 7)) & 1u) == 0u) s[i] = -INFINITY;
+    bf16x8 pb[2];
+    softmax(pb, s, a.c);
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+      for (int jt = 0; jt < D / 32; ++jt) {
+        bf16x8 v;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = vx[kk][e][jt];
+        o[jt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, pb[kk], o[jt], 0, 0, 0);
+      }
   }
   // Tiles first, first + stride, .. below `end` of the prefix.  (Requests past the end ask for the last tile again: a branch
   // would make every wait one for everything in flight.)
-  __device__ void run(const TiledArgs& a, const int32_t* table, int g, int first, int end, int stride, int len, int lane) {
-    if (first >= end) return;
+  // `between` runs while the first requests are on their way.
+  template <typename Between>
+  __device__ void run(const TiledArgs& a, const int32_t* table, int g, int first, int end, int stride, int len, int lane, Between between) {
+    if (first >= end) {  // (apart, or the loop's waits allow for requests that were never made)
+      between();
+      return;
+    }
     const uint8_t* kc = (const uint8_t*)a.k_cache + (int64_t)g * a.head_stride;
     const uint8_t* vc = (const uint8_t*)a.v_cache + (int64_t)g * a.head_stride;
     Ids id[2];
@@ -886,6 +946,7 @@ struct Fp4Stream {
     request_ids(1, first + stride);
     request(0, first);
     request(1, first + stride);
+    between();
     // All but the last one or two in pairs (no way out of a pair: where one can be left between its tiles, the waits of both
     // are for everything in flight).  Only the wavefront's last tile can be the one that the prefix ends in.
     const int pairs = ((end - 1 - first) / stride) / 2;
@@ -1166,6 +1227,7 @@ __device__ inline void zero_row(const TiledArgs& a, int64_t row, int e) {
 template <typename T, CacheType kCache, bool kPlain, int D, bool kDirect>
 __global__ __launch_bounds__(kThreads, 2) void tva_tiled_kernel(TiledArgs a) {
   typedef Stager<T, kCache, kPlain, D> Stage;
+  constexpr bool kStream = streams<T>(kCache, D);
   constexpr int kStepKeys = step_keys<T>();
   constexpr int kRegion = region_floats(D);
   constexpr int kStageBytes = 2 * 2 * Stage::kStepChunks * 16, kFoldBytes = kWaves * kRegion * 4;
@@ -1304,23 +1366,24 @@ __global__ __launch_bounds__(kThreads, 2) void tva_tiled_kernel(TiledArgs a) {
       const int r = (group_rows + kRowTile - 1) / kRowTile;
       // row tile, first tile of a step and stride between tiles of this wavefront; wavefronts rt, rt + apart, ... share one
       const int apart = r >= 3 ? 4 : r;
-      // a 4-bit cache and one row tile: every wavefront streams tiles of its own
-      const bool stream = kCache == kE2M1 && sizeof(T) == 2 && D == 128 && r == 1;
-      const int shared = stream ? kWaves : (r >= 3 ? 2 : 4);  // wavefronts per row tile
+      // streams: the wavefronts of a row tile share its keys
+      const int shared = kStream ? kWaves / apart : (r >= 3 ? 2 : 4);  // wavefronts per row tile
       const int rt = wv & (apart - 1), first = r == 1 ? wv : (r == 2 ? wv >> 1 : wv >> 2);
-      const bool busy = rt < r && first < kTilesPerStep;
+      const bool busy = rt < r && (kStream || first < kTilesPerStep);
       const int32_t* table = a.block_table + (int64_t)b * a.max_blocks;
       float* regions = (float*)lds;
-      if constexpr (kCache == kE2M1 && sizeof(T) == 2 && D == 128) {
-        if (stream) {
-          Fp4Stream st;
-          st.begin(a, sh.base, g, row0, rows, lane);
-          st.run(a, table, g, t0 * kTilesPerStep + wv, min(t1 * kTilesPerStep, (len + 31) / 32), kWaves, len, lane);
-          __syncthreads();  // the piece before is done with the LDS
-          st.put(regions + wv * kRegion, lane);
-        }
-      }
-      if (!stream) {
+      if constexpr (kStream) {
+        Fp4Stream st;
+        const int my_row0 = row0 + (busy ? rt * kRowTile : 0);
+        st.begin(a, sh.base, g, my_row0, rows, lane);
+        const bool ends = t1 == sh.steps;  // the piece that ends the segment has the tree part too
+        if (busy)
+          st.run(a, table, g, t0 * kTilesPerStep + first, min(t1 * kTilesPerStep, (len + 31) / 32), shared, len, lane, [&]() {
+            for (int tt = first; ends && tt * 32 < sh.n; tt += shared) st.tree_tile(a, g, sh.base, sh.n, my_row0, rows, tt, lane);
+          });
+        __syncthreads();  // the piece before is done with the LDS
+        st.put(regions + wv * kRegion, lane);
+      } else {
         Rows<T, kPlain, D> rowset;
         rowset.begin(a, sh.base, g, row0 + (busy ? rt * kRowTile : 0), rows, lane);
         Stage st;
@@ -1391,8 +1454,8 @@ __global__ __launch_bounds__(kThreads, 2) void tva_tiled_kernel(TiledArgs a) {
           const int node = sh.base + rho / a.G, head = g * a.G + rho % a.G;
           Finish<T, D> f;
           f.request(a, node, head, active, e);
-          f.tree(a, g, sh.base, sh.n, e);
-          if (active && t0 < t1)
+          f.tree(a, g, sh.base, kStream ? 0 : sh.n, e);
+          if (active && (kStream || t0 < t1))
             f.merge(f.fetch(s_ml[0][i] * a.m_scale, s_ml[1][i], regions + (i >> 5) * kRegion + (i & 31) * 4, kRowTile * 4, e),
                     a.c);
           if (active) f.write(a, node, head, e);
@@ -1471,7 +1534,7 @@ __global__ __launch_bounds__(finish_waves(kParts) * kWave, kParts == 0 ? 2 : 1) 
   const Shape sh = shape_of<T>(a, a.prefix_len[b], a.cu_nodes[b], a.cu_nodes[b + 1]);
   const bool owned = there && node >= sh.base && (int64_t)node - sh.base < sh.n;
   const int64_t units_before = a.plan[2 + b], segs_before = a.plan[2 + a.batch + b];
-  if (part < 0) f.tree(a, g, sh.base, owned ? sh.n : 0, e);
+  if (part < 0) f.tree(a, g, sh.base, owned && !(a.stream && sh.steps > 0) ? sh.n : 0, e);
   if ((kParts == 0 || part >= 0) && owned && sh.steps > 0 && U > 0) {
     const int rho = (node - sh.base) * a.G + head % a.G;
     const int group = rho / kGroupRows, r = rho % kGroupRows, local = g * sh.groups + group;
@@ -1663,6 +1726,7 @@ int32_t tva_launch_tiled(smart_ctx* ctx, hipStream_t stream, const tva_params& p
   a.segment_cost = segment_cost(p, tiled_workgroups(ctx));
   a.fp8 = fp8;
   a.fp4 = fp4;
+  a.stream = fp4 && !f32 && streams<__bf16>(kE2M1, p.head_dim);
   a.plain = p.kv_layout == SMART_KV_PLAIN;
   // t8 / d as the high word of 2 t8 * (floor(2^31 / d) + 1): exact for t8 < 2^28 and d <= 8
   a.block8_magic = (uint32_t)((1ull << 31) / ((uint32_t)p.block_size / 8)) + 1u;
