@@ -1682,8 +1682,17 @@ int32_t tva_launch_tiled(smart_ctx* ctx, hipStream_t stream, const tva_params& p
   // token, 16-node trees, 14.7 .. 15.5 us in fp32 where the general kernel takes 12.8 .. 13.8; from 8 tokens on it is behind.
   const int64_t longest = (int64_t)p.max_blocks_per_seq * p.block_size;
   const int64_t step = f32 ? step_keys<float>() : step_keys<__bf16>(), rows = (int64_t)p.total_nodes * G;
+  // Where the operands stream from 4-bit pages a step is cheaper, and a workgroup takes as long as its keys times its rows
+  // (up to 32 of them cost the same).  32 / 8 heads of 128, split and direct: one sequence, 8 nodes (32 rows), 517 tokens
+  // 16.7 / 12.1 us, 1500 17.6 / 16.0, 2050 19.5 / 18.7, 3000 21.1 / 22.5; 16 nodes, 800 tokens 18.1 / 16.8, 1030 18.9 / 19.2; 32
+  // nodes, 260 tokens 18.7 / 16.3, 517 19.9 / 20.7.  8 sequences: 2050 20.3 / 19.0, 1030 25.5 / 19.5, 517 29.3 / 21.3.  30: 8 nodes
+  // 1030 29.2 / 28.6, 2050 34.3 / 37.6, single tokens (29 segments of 4 rows a head) 30.8 / 19.5; 16 nodes 1030 37.4 / 38.1; 32 nodes 517
+  // 45.4 / 41.9.
+  const bool stream4 = fp4 && !f32 && streams<__bf16>(kE2M1, p.head_dim);
+  const int64_t mean_rows = (rows + p.batch - 1) / p.batch;
   const bool few_steps = (longest <= step && rows <= 384 * (int64_t)p.batch) ||
-                         (!f32 && longest <= 4 * step && rows <= 64 * (int64_t)p.batch);
+                         (!f32 && longest <= 4 * step && rows <= 64 * (int64_t)p.batch) ||
+                         (stream4 && longest * (mean_rows > 32 ? mean_rows : 32) <= 65536);
   bool direct = fixed != nullptr || (few_steps && segs <= (ctx->num_cus > 0 ? ctx->num_cus : 256));
   if (!direct) {
     hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
@@ -1726,7 +1735,7 @@ int32_t tva_launch_tiled(smart_ctx* ctx, hipStream_t stream, const tva_params& p
   a.segment_cost = segment_cost(p, tiled_workgroups(ctx));
   a.fp8 = fp8;
   a.fp4 = fp4;
-  a.stream = fp4 && !f32 && streams<__bf16>(kE2M1, p.head_dim);
+  a.stream = stream4;
   a.plain = p.kv_layout == SMART_KV_PLAIN;
   // t8 / d as the high word of 2 t8 * (floor(2^31 / d) + 1): exact for t8 < 2^28 and d <= 8
   a.block8_magic = (uint32_t)((1ull << 31) / ((uint32_t)p.block_size / 8)) + 1u;
