@@ -829,8 +829,9 @@ int32_t tree_commit_fp4(smart_ctx* ctx, void* stream, int32_t src_dtype,
  * written.  Uses no workspace: it may be captured, and calls may overlap.
  * Host errors: SMART_EINVAL for null pointers, Hq % Hkv != 0, head_dim not in
  * {64, 128}, unknown dtype, softmax_scale not positive or not below 1e30,
- * total_tokens x Hq >= 2^31, token strides smaller than a token's row, pointers or
- * token strides that are not multiples of 16 bytes; SMART_EHIP.
+ * total_tokens x Hq >= 2^31, token strides smaller than a token's row, k_stride or
+ * v_stride of 2^24 elements or more, pointers or token strides that are not multiples
+ * of 16 bytes; SMART_EHIP.
  * ------------------------------------------------------------------------- */
 typedef struct {
   int32_t dtype; /* SMART_F32 | SMART_BF16: q, k, v, out share it */

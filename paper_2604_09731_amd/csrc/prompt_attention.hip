@@ -1,11 +1,11 @@
 // prompt_attention: causal attention of packed prompts, the prefill that lays down what tree_verify_attention streams.
 //
 // Per (prompt, kv head g) the rows are (token, query head of the group) pairs, rho = token * G + head, so that the heads that
-// share keys share the key tiles, and a row tile spans few tokens (few keys behind the diagonal).  A workgroup takes kRows
-// consecutive rows, a wavefront 32 R of them, and streams the keys up to its last token past them: one pass with the running
-// maximum and sum of a softmax, keys and values staged through LDS.
-//   * Scores are kept transposed (keys x rows): a row's softmax stays inside a lane and its partner in the other half of
-//     the wavefront, and the probabilities come out in the operand layout of the second product.
+// share keys share the key tiles, and a row tile spans few tokens (few keys behind the diagonal).  A workgroup takes
+// consecutive rows, a wavefront 16 or a few times 16 of them, and streams the keys up to its last token past them, 64 at a
+// time: one pass with the running maximum and sum of a softmax, keys and values staged through LDS.
+//   * Scores are kept transposed (keys x rows): a row's softmax stays inside the four lanes of a column, and the
+//     probabilities come out in the operand layout of the second product.
 //   * Row tiles are handed out from the longest down: what is dispatched last is short.
 //   * Bound by the matrix cores: 4 D flops per (row, key).
 //   * Values of later tokens are multiplied by probabilities of zero where a tile crosses the diagonal; if that makes a row
@@ -23,12 +23,10 @@ typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 typedef __attribute__((ext_vector_type(4))) short shortx4;
 typedef __attribute__((ext_vector_type(4))) float floatx4;
 typedef __attribute__((ext_vector_type(8))) float floatx8;
-typedef __attribute__((ext_vector_type(16))) float floatx16;
 typedef __attribute__((ext_vector_type(4))) uint32_t uintx4;
 typedef __attribute__((address_space(3))) shortx4 lds_shortx4;
 
 constexpr int kWave = 64;
-constexpr int kTile = 32;  // keys and rows of a score tile
 constexpr float kLog2e = 1.4426950408889634f;
 // The reference of the exponentials follows the running maximum only when that has moved more than 2^kRescaleStep above it.
 constexpr float kRescaleStep = 8.f;
@@ -55,14 +53,20 @@ __device__ inline float sum_halves(float x) {
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
+__device__ inline float max_quarters(float x) {  // over the lanes with the same lane % 16
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return max_halves(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
+}
+__device__ inline float sum_quarters(float x) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return sum_halves(__uint_as_float(r[0]) + __uint_as_float(r[1]));
+}
+
 __device__ inline int wave_sum(int v) {
   int64_t total;
   smart::wave_excl_scan(v, threadIdx.x & (kWave - 1), &total);
   return (int)total;
 }
-
-// Key (of 32) that register r of a lane in half h holds.
-__device__ inline int key_of(int r, int h) { return 8 * (r >> 2) + 4 * h + (r & 3); }
 
 // ---- which rows a workgroup takes ------------------------------------------------------------------------------------
 struct Item {
@@ -155,19 +159,30 @@ template <typename T, int D, int kThreads>
 struct Stage {
   static constexpr int kE = 16 / (int)sizeof(T);
   static constexpr int kRowChunks = D / kE;
-  static constexpr int kKeys = sizeof(T) == 2 ? 64 : 32;
+  static constexpr int kKeys = 64;
   static constexpr int kChunks = kKeys * kRowChunks;  // of K, and of V
   static constexpr int kPer = kChunks / kThreads;
   uintx4 k[kPer], v[kPer];
 
-  // Rows past the prompt's end repeat its last one (their scores are masked).
-  __device__ void load(const T* kp, const T* vp, const PromptArgs& a, int key0, int len, int tid) {
+  uint32_t ko[kPer], vo[kPer];  // bytes from a stage's first row (check keeps strides below 2^24 elements)
+
+  // The rows of a stage, of which `rows` exist: those past the prompt's end repeat its last one (their scores are masked).
+  __device__ void place(const PromptArgs& a, int rows, int tid) {
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
-      const int p = i * kThreads + tid, key = p / kRowChunks, c = (p % kRowChunks) ^ swizzle<T, D>(key);
-      const int64_t t = min(key0 + key, len - 1);
-      k[i] = *(const uintx4*)(kp + t * a.k_stride + c * kE);
-      v[i] = *(const uintx4*)(vp + t * a.v_stride + c * kE);
+      const int p = i * kThreads + tid, key = p / kRowChunks, c = (p % kRowChunks) ^ swizzle<T, D>(key), row = min(key, rows - 1);
+      ko[i] = ((uint32_t)row * (uint32_t)a.k_stride + c * kE) * (uint32_t)sizeof(T);
+      vo[i] = ((uint32_t)row * (uint32_t)a.v_stride + c * kE) * (uint32_t)sizeof(T);
+    }
+  }
+  // Stages are requested in order; the last one may be short.
+  __device__ void load(const T* kp, const T* vp, const PromptArgs& a, int key0, int len, int tid) {
+    if (key0 == 0 || key0 + kKeys > len) place(a, len - key0, tid);
+    const char *kb = (const char*)(kp + key0 * a.k_stride), *vb = (const char*)(vp + key0 * a.v_stride);
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      k[i] = *(const uintx4*)(kb + ko[i]);
+      v[i] = *(const uintx4*)(vb + vo[i]);
     }
   }
   __device__ void store(uintx4* lds, int tid) const {
@@ -175,40 +190,6 @@ struct Stage {
     for (int i = 0; i < kPer; ++i) {
       lds[i * kThreads + tid] = k[i];
       lds[kChunks + i * kThreads + tid] = v[i];
-    }
-  }
-};
-
-// ---- the two products of a wavefront's rows with 32 staged keys ----------------------------------------------------------
-template <int D>
-struct ProductsF32 {
-  typedef floatx4 Query[D / 8];
-  static constexpr int kRowChunks = D / 4;
-  __device__ static void load_query(Query& q, const float* row, int h) {
-#pragma unroll
-    for (int s = 0; s < D / 8; ++s) q[s] = *(const floatx4*)(row + 8 * s + 4 * h);
-  }
-  __device__ static floatx16 scores(const uintx4* kt, const Query& q, int lane) {
-    const int h = lane >> 5, j = lane & 31;
-    floatx16 s = (floatx16)(0.f);
-#pragma unroll
-    for (int x = 0; x < D / 8; ++x) {  // contraction step (x, e): the halves hold head dims 8 x + e and 8 x + 4 + e
-      const floatx4 k = __builtin_bit_cast(floatx4, kt[j * kRowChunks + ((2 * x + h) ^ swizzle<float, D>(j))]);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_32x32x2f32(k[e], q[x][e], s, 0, 0, 0);
-    }
-    return s;
-  }
-  __device__ static void output(floatx16 (&o)[D / 32], const uintx4* vt, const floatx16& p, int lane) {
-    const int h = lane >> 5, j = lane & 31;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {  // register i of the halves: two keys
-      const int key = key_of(i, h);
-#pragma unroll
-      for (int jt = 0; jt < D / 32; ++jt) {
-        const float v = ((const float*)(vt + key * kRowChunks + ((8 * jt + (j >> 2)) ^ swizzle<float, D>(key))))[j & 3];
-        o[jt] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, p[i], o[jt], 0, 0, 0);
-      }
     }
   }
 };
@@ -246,31 +227,42 @@ __device__ void walk(const PromptArgs& a, int base, int token, int head, int lan
 }
 
 // ---- fp32 -----------------------------------------------------------------------------------------------------------------
+// A wavefront's 16 rows against 32 staged keys, in 16 x 16 tiles.  Lane (quarter w, i) of a score tile: row i and keys 4 w + 0 ..
+// 3, which are the ones it contributes to the output product, register by register.  Both products contract over what 16-byte
+// reads bring: a score's step (x, e) over the head dims 16 x + 4 w + e, and row i of output tile (x, e) is head dim 64 x + 4 i + e.
+// Two wavefronts share rows and take the two halves of every stage, so that a compute unit has two on each matrix core even
+// where it has one row tile, and a long prompt's last tile, which nothing can follow, takes half as long.  8 / 2 heads of 64:
+// 6600 tokens of 8 prompts 106 us (98 TFLOP/s; with 32 x 32 tiles, 128 rows and no sharing 148; 64 rows without sharing 110), one
+// prompt of 1536 62 (129, 72), of 300 16.6 (29, 17.7), 4 of 4096 571 (653, 579); head dim 128, 4 of 2048 324 (335, 341).  Left without
+// the softmax it takes 6 % less, without staging 8 %; the rest is what the ends of the row tiles leave idle.
 template <int D>
-__global__ __launch_bounds__(256, 1) void prompt_f32_kernel(PromptArgs a) {
-  constexpr int kThreads = 256, kRows = kThreads / kWave * kTile;
-  typedef ProductsF32<D> P;
+__global__ __launch_bounds__(512, D == 64 ? 4 : 2) void prompt_f32_kernel(PromptArgs a) {
+  constexpr int kThreads = 512, kTileRows = 16, kRowWaves = kThreads / kWave / 2, kRows = kRowWaves * kTileRows;
   typedef Stage<float, D, kThreads> S;
   __shared__ uintx4 lds[2][2 * S::kChunks];
-  const int tid = threadIdx.x, lane = tid & (kWave - 1), h = lane >> 5, j = lane & 31;
-  const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int tid = threadIdx.x, lane = tid & (kWave - 1), w = lane >> 4, i16 = lane & 15;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wv = wave % kRowWaves, part = wave / kRowWaves;
   const int g = blockIdx.x % a.Hkv, rank = blockIdx.x / a.Hkv;
   const Item it = find_item<kRows, kThreads>(a, rank);
   if (it.tile < 0 || it.len <= 0) return;
   const int base = __builtin_amdgcn_readfirstlane(it.base), len = __builtin_amdgcn_readfirstlane(it.len);
   const int rows = len * a.G, row0 = __builtin_amdgcn_readfirstlane(it.tile) * kRows;
-  const int mine = row0 + wv * kTile;                        // this wavefront's first row
+  const int mine = row0 + wv * kTileRows;                    // this wavefront's first row
   const int keys = (min(row0 + kRows, rows) - 1) / a.G + 1;  // keys of the workgroup
-  const int last = (min(mine + kTile, rows) - 1) / a.G;      // the last key of the wavefront (with rows)
+  const int last = (min(mine + kTileRows, rows) - 1) / a.G;  // the last key of the wavefront (with rows)
   const int first = min(mine, rows - 1) / a.G;               // and its first token
 
-  const int rho = min(mine + j, rows - 1);  // padding rows repeat the last real row; never written
+  const int rho = min(mine + i16, rows - 1);  // padding rows repeat the last real row; never written
   const int token = rho / a.G, head = g * a.G + rho % a.G;
-  typename P::Query q;
-  P::load_query(q, (const float*)a.q + (int64_t)(base + token) * a.q_stride + (int64_t)head * D, h);
-  floatx16 o[D / 32];
+  floatx4 q[D / 16];
 #pragma unroll
-  for (int jt = 0; jt < D / 32; ++jt) o[jt] = (floatx16)(0.f);
+  for (int x = 0; x < D / 16; ++x)
+    q[x] = *(const floatx4*)((const float*)a.q + (int64_t)(base + token) * a.q_stride + (int64_t)head * D + 16 * x + 4 * w);
+  floatx4 o[D / 64][4];
+#pragma unroll
+  for (int x = 0; x < D / 64; ++x)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[x][e] = (floatx4)(0.f);
   float m = -INFINITY, l = 0.f;
   const float* kp = (const float*)a.k + (int64_t)base * a.k_stride + (int64_t)g * D;
   const float* vp = (const float*)a.v + (int64_t)base * a.v_stride + (int64_t)g * D;
@@ -282,52 +274,97 @@ __global__ __launch_bounds__(256, 1) void prompt_f32_kernel(PromptArgs a) {
     stage.store(at, tid);
     if (t + 1 < steps) stage.load(kp, vp, a, (t + 1) * S::kKeys, len, tid);
     __syncthreads();  // the stage is full, and everyone is done with the other one
-    const int key0 = t * S::kKeys;
+    const int key0 = t * S::kKeys + 32 * part;
+    const uintx4 *kt0 = at + 32 * part * S::kRowChunks, *vt = kt0 + S::kChunks;
     if (mine >= rows || key0 > last) continue;
-    floatx16 s = P::scores(at, q, lane);
-    if (key0 + kTile - 1 > first) {
+    floatx4 s[2];
+    s[0] = s[1] = (floatx4)(0.f);
 #pragma unroll
-      for (int i = 0; i < 16; ++i)
-        if (key0 + key_of(i, h) > token) s[i] = -INFINITY;
+    for (int x = 0; x < D / 16; ++x) {
+      floatx4 k[2];
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt)
+        k[kt] = __builtin_bit_cast(floatx4, kt0[(16 * kt + i16) * S::kRowChunks + ((4 * x + w) ^ swizzle<float, D>(16 * kt + i16))]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt) s[kt] = __builtin_amdgcn_mfma_f32_16x16x4f32(k[kt][e], q[x][e], s[kt], 0, 0, 0);
     }
-    float mx = s[0];
+    if (key0 + 31 > first) {
 #pragma unroll
-    for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[i]);
-    const float m_new = fmaxf(m, max_halves(mx));
+      for (int r = 0; r < 8; ++r)
+        if (key0 + 16 * (r >> 2) + 4 * w + (r & 3) > token) s[r >> 2][r & 3] = -INFINITY;
+    }
+    float mx = s[0][0];
+#pragma unroll
+    for (int r = 1; r < 8; ++r) mx = fmaxf(mx, s[r >> 2][r & 3]);
+    const float m_new = fmaxf(m, max_quarters(mx));
     if (__any((m_new - m) * a.c > kRescaleStep)) {
       const float alpha = __builtin_amdgcn_exp2f((m - (m_new == -INFINITY ? 0.f : m_new)) * a.c);
       l *= alpha;
 #pragma unroll
-      for (int jt = 0; jt < D / 32; ++jt) o[jt] *= alpha;
+      for (int x = 0; x < D / 64; ++x)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[x][e] *= alpha;
       m = m_new;
     }
     const float mc = m == -INFINITY ? 0.f : m * a.c;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], a.c, -mc));
-      l += s[i];
+    for (int r = 0; r < 8; ++r) {
+      const float p = __builtin_amdgcn_exp2f(fmaf(s[r >> 2][r & 3], a.c, -mc));
+      s[r >> 2][r & 3] = p;
+      l += p;
     }
-    P::output(o, at + S::kChunks, s, lane);
+#pragma unroll
+    for (int r = 0; r < 8; ++r) {
+      const int key = 16 * (r >> 2) + 4 * w + (r & 3);
+#pragma unroll
+      for (int x = 0; x < D / 64; ++x) {
+        const floatx4 v = __builtin_bit_cast(floatx4, vt[key * S::kRowChunks + ((16 * x + i16) ^ swizzle<float, D>(key))]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[x][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[e], s[r >> 2][r & 3], o[x][e], 0, 0, 0);
+      }
+    }
   }
-  if (mine >= rows) return;
-  const bool there = mine + j < rows;
-  const float sum = sum_halves(l), inv = sum > 0.f ? 1.f / sum : 0.f;
+  // The odd halves of the stages join the even ones.
+  __syncthreads();
+  floatx4* const mo = (floatx4*)lds[0];
+  float* const ml = (float*)(mo + D / 16 * kRowWaves * kWave);
+  const int at = wv * kWave + lane;
+  if (part) {
+#pragma unroll
+    for (int x = 0; x < D / 16; ++x) mo[x * kRowWaves * kWave + at] = o[x / 4][x % 4];
+    ml[at] = m;
+    ml[kRowWaves * kWave + at] = l;
+  }
+  __syncthreads();
+  if (part || mine >= rows) return;
+  const float m2 = ml[at], top = fmaxf(m, m2);
+  const float w1 = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - top) * a.c);
+  const float w2 = m2 == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m2 - top) * a.c);
+  l = l * w1 + ml[kRowWaves * kWave + at] * w2;
+  m = top;
+#pragma unroll
+  for (int x = 0; x < D / 16; ++x) o[x / 4][x % 4] = o[x / 4][x % 4] * w1 + mo[x * kRowWaves * kWave + at] * w2;
+  const bool there = mine + i16 < rows;
+  const float sum = sum_quarters(l), inv = sum > 0.f ? 1.f / sum : 0.f;
   float bad = 0.f;
 #pragma unroll
-  for (int jt = 0; jt < D / 32; ++jt)
+  for (int x = 0; x < D / 64; ++x)
 #pragma unroll
-    for (int i4 = 0; i4 < 4; ++i4) {
-      floatx4 x;
+    for (int r = 0; r < 4; ++r) {  // row 4 w + r of the four tiles
+      floatx4 y;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        x[i] = o[jt][4 * i4 + i] * inv;
-        bad = fmaf(x[i], 0.f, bad);
+      for (int e = 0; e < 4; ++e) {
+        y[e] = o[x][e][r] * inv;
+        bad = fmaf(y[e], 0.f, bad);
       }
-      if (there) *(floatx4*)((float*)a.out + (int64_t)(base + token) * a.out_stride + (int64_t)head * D + 32 * jt + 8 * i4 + 4 * h) = x;
+      if (there)
+        *(floatx4*)((float*)a.out + (int64_t)(base + token) * a.out_stride + (int64_t)head * D + 64 * x + 16 * w + 4 * r) = y;
     }
-  if (a.lse && there && h == 0) a.lse[(int64_t)(base + token) * a.Hq + head] = sum > 0.f ? m * a.scale + logf(sum) : -INFINITY;
+  if (a.lse && there && w == 0) a.lse[(int64_t)(base + token) * a.Hq + head] = sum > 0.f ? m * a.scale + logf(sum) : -INFINITY;
   uint64_t again = __ballot(there && bad != 0.f && sum < INFINITY);
-  again = (again | again >> 32) & 0xFFFFFFFFull;
+  again = (again | again >> 16 | again >> 32 | again >> 48) & 0xFFFFull;
   for (; again; again &= again - 1) {
     const int row = mine + __ffsll((unsigned long long)again) - 1;
     walk<float, D>(a, base, row / a.G, g * a.G + row % a.G, lane);
@@ -339,15 +376,6 @@ __global__ __launch_bounds__(256, 1) void prompt_f32_kernel(PromptArgs a) {
 __device__ inline float add_pair(uint32_t pair, float sum) {
   return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pair), __builtin_bit_cast(bf16x2, 0x3F803F80u), sum, false);
 }
-__device__ inline float max_quarters(float x) {  // over the lanes with the same lane % 16
-  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return max_halves(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
-}
-__device__ inline float sum_quarters(float x) {
-  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return sum_halves(__uint_as_float(r[0]) + __uint_as_float(r[1]));
-}
-
 __device__ inline float highest(const floatx8& x) {
   return fmaxf(fmaxf(fmaxf(fmaxf(x[0], x[1]), x[2]), fmaxf(x[3], x[4])), fmaxf(fmaxf(x[5], x[6]), x[7]));
 }
@@ -662,6 +690,8 @@ int32_t check(const prompt_params& p) {
   if ((int64_t)p.total_tokens * p.num_q_heads > 0x7FFFFFFF) return SMART_EINVAL;
   const int64_t unit = p.dtype == SMART_F32 ? 4 : 8, q_row = (int64_t)p.num_q_heads * p.head_dim, kv_row = (int64_t)p.num_kv_heads * p.head_dim;
   if (p.q_stride < q_row || p.out_stride < q_row || p.k_stride < kv_row || p.v_stride < kv_row) return SMART_EINVAL;
+  // (rows of a stage, 64 of them, are addressed in 32 bits)
+  if (p.k_stride >= (1 << 24) || p.v_stride >= (1 << 24)) return SMART_EINVAL;
   if (p.q_stride % unit || p.k_stride % unit || p.v_stride % unit || p.out_stride % unit) return SMART_EINVAL;
   if (p.batch == 0 || p.total_tokens == 0) return SMART_OK;
   if (!p.d_q || !p.d_k || !p.d_v || !p.d_cu_tokens || !p.d_out) return SMART_EINVAL;
@@ -699,7 +729,7 @@ extern "C" int32_t prompt_attention(smart_ctx* ctx, void* stream, const prompt_p
   if (prev != ctx->device) SMART_HIP_CHECK(hipSetDevice(ctx->device));
   hipStream_t s = (hipStream_t)stream;
   if (p.dtype == SMART_F32) {
-    rc = p.head_dim == 128 ? launch(prompt_f32_kernel<128>, 256, 128, a, s) : launch(prompt_f32_kernel<64>, 256, 128, a, s);
+    rc = p.head_dim == 128 ? launch(prompt_f32_kernel<128>, 512, 64, a, s) : launch(prompt_f32_kernel<64>, 512, 64, a, s);
   } else {
     rc = p.head_dim == 128 ? launch_bf16<128>(ctx, a, s) : launch_bf16<64>(ctx, a, s);
   }

@@ -26,7 +26,7 @@ def _prompt(**kw):
 @pytest.mark.parametrize("bad", [
     dict(dtype=2), dict(batch=-1), dict(total_tokens=-1), dict(num_q_heads=0), dict(num_kv_heads=0), dict(num_kv_heads=3),
     dict(head_dim=96), dict(head_dim=0), dict(softmax_scale=0.0), dict(softmax_scale=float("nan")), dict(softmax_scale=1e30),
-    dict(total_tokens=1 << 28), dict(q_stride=504), dict(out_stride=511), dict(k_stride=127), dict(v_stride=64),
+    dict(total_tokens=1 << 28), dict(q_stride=504), dict(out_stride=511), dict(k_stride=127), dict(v_stride=64), dict(k_stride=1 << 24), dict(v_stride=1 << 24),
     dict(q_stride=516), dict(k_stride=132), dict(v_stride=129), dict(out_stride=1028), dict(d_q=None), dict(d_k=None),
     dict(d_v=None), dict(d_out=None), dict(d_cu_tokens=None), dict(d_q=AT + 8), dict(d_k=AT + 2), dict(d_v=AT + 4), dict(d_out=AT + 8),
 ])

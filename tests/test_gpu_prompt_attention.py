@@ -265,3 +265,20 @@ def test_the_last_row_of_a_large_call_is_reached(lib):
     out, lse = lib.prompt_attention(q, k, k, cu, 0.125, want_lse=True)
     c = lambda x: x[-tail:].contiguous()
     _check(c(out), c(lse), c(q), c(k), c(k), np.array([0, tail], np.int32), 0.125, "bf16")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rows_far_apart(lib, dtype):
+    """Offsets between the 64 keys of a stage that need all of 32 bits, and beyond them 64."""
+    import torch
+    cu, D, stride = np.array([0, 3, 133], np.int32), 64, (1 << 24) - 8
+    q, k, v = _inputs(133, 2, 1, D, dtype, 9)
+    store = torch.empty(132 * stride + 2 * D, dtype=q.dtype, device="cuda")       # 4.4 or 8.9 GB
+    far = [store.as_strided((133, 1, D), (stride, D, 1), o) for o in (0, D)]
+    far[0].copy_(k)
+    far[1].copy_(v)
+    out, lse = lib.prompt_attention(q, *far, torch.from_numpy(cu).cuda(), D ** -0.5, want_lse=True)
+    near = lib.prompt_attention(q, k, v, torch.from_numpy(cu).cuda(), D ** -0.5, want_lse=True)
+    assert torch.equal(out, near[0]) and torch.equal(lse, near[1])
+    with pytest.raises(B.SmartError):
+        lib.prompt_attention(q[:2], store.as_strided((2, 1, D), (1 << 24, D, 1)), v[:2], torch.tensor([0, 2], dtype=torch.int32).cuda(), 1.0)
