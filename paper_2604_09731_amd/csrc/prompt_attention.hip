@@ -42,6 +42,7 @@ struct PromptArgs {
   const int32_t* cu;
   int64_t q_stride, k_stride, v_stride, out_stride;
   int32_t batch, total_tokens, Hq, Hkv, G;
+  uint32_t num_cus;
   float scale, c;  // c: in powers of two
 };
 
@@ -565,7 +566,11 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void prompt_bf16_kernel(PromptArg
   const int tid = threadIdx.x, lane = tid & (kWave - 1);
   const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
   // consecutive workgroups go to different L2s: the row tiles of one kv head sit behind as few of them as possible
-  const int g = blockIdx.x % a.Hkv, rank = blockIdx.x / a.Hkv;
+  uint32_t id = blockIdx.x;
+  // Where two workgroups share a compute unit the second one on each is as long as the first is short: 32 / 8 heads, one prompt of
+  // 2048 tokens 57.3 us in order, 51.8 so; of 1024 24.5 and 23.0; 8262 tokens of five 165 and 160.
+  if (kWaves == 4 && id >= a.num_cus && id < 2 * a.num_cus && 2 * a.num_cus <= gridDim.x) id = 3 * a.num_cus - 1 - id;
+  const int g = id % a.Hkv, rank = id / a.Hkv;
   const Item it = find_item<kRows, kThreads>(a, rank);
   if (it.tile < 0 || it.len <= 0) return;
   const int base = __builtin_amdgcn_readfirstlane(it.base), len = __builtin_amdgcn_readfirstlane(it.len);
@@ -670,13 +675,15 @@ int32_t launch_rows(const PromptArgs& a, hipStream_t stream) {
 
 // Taller row tiles read the LDS less often per product, but there have to be enough of them to fill the chip and to let the short
 // ones fill in behind the long.  us with tiles of 64 / 128 / 256 rows (four wavefronts; 256 rows of head dim 128 eight), 32 / 8
-// heads: one prompt of 37 tokens 5.3 / 6.3 / 6.9, of 512 14.4 / 18.6 / 23; 4 of 512 26.7 / 22.3 / 26; one of 2048 70 / 59 / 64; 8262
-// tokens 256 / 172.9 / 171.8; 16384 tokens, 64 heads 6633 / 4307 / 3831; head dim 64, 64 prompts of 1 .. 300 tokens, 8 heads 14.1 /
-// 12.1 / 14.8, 4 of 4096 420 / 325 / 301.
+// heads: one prompt of 37 tokens 5.2 / 6.6 / 7.9, of 512 13.2 / 17.8 / 22.3, of 1500 36.2 / 43.5 / 47.0, of 2048 57.1 / 52.7 / 61.3, of
+// 4096 194 / 140 / 133; 12 of 341 .. 1024 92.6 / 70.7 / 73.5; 8262 tokens of five 223 / 166 / 165; 16384 tokens, 64 heads 5647 / 3987 /
+// 3690; head dim 64, 8 heads, one of 4096 34.6 / 46.1 / 74.0, 64 of 1 .. 300 14.7 / 11.7 / 14.9, 4 of 1024 .. 2048 26.4 / 34.3 / 52.4;
+// 32 heads, 4 of 4096 383 / 309 / 289.  (Two teams of wavefronts on one row tile, with half of the keys each, are ahead for a few
+// prompts of few heads only: one of 4096, 8 heads of 64, 27 for 35 us; one of 2048, 32 heads of 128, 51; 8262 tokens 212.)
 template <int D>
-int32_t launch_bf16(const smart_ctx* ctx, const PromptArgs& a, hipStream_t stream) {
-  const int64_t rows = (int64_t)a.total_tokens * a.Hq, cus = ctx->num_cus > 0 ? ctx->num_cus : 256;
-  if (rows <= 128 * cus) return launch_rows<D, 4, 1>(a, stream);
+int32_t launch_bf16(const PromptArgs& a, hipStream_t stream) {
+  const int64_t rows = (int64_t)a.total_tokens * a.Hq, cus = a.num_cus;
+  if (rows <= 192 * cus) return launch_rows<D, 4, 1>(a, stream);
   if (rows < 4 * 256 * cus) return launch_rows<D, 4, 2>(a, stream);
   return launch_rows<D, D == 128 ? 8 : 4, D == 128 ? 2 : 4>(a, stream);
 }
@@ -722,6 +729,7 @@ extern "C" int32_t prompt_attention(smart_ctx* ctx, void* stream, const prompt_p
   a.Hq = p.num_q_heads;
   a.Hkv = p.num_kv_heads;
   a.G = p.num_q_heads / p.num_kv_heads;
+  a.num_cus = ctx->num_cus > 0 ? ctx->num_cus : 256;
   a.scale = p.softmax_scale;
   a.c = p.softmax_scale * kLog2e;
   int prev = 0;
@@ -731,7 +739,7 @@ extern "C" int32_t prompt_attention(smart_ctx* ctx, void* stream, const prompt_p
   if (p.dtype == SMART_F32) {
     rc = p.head_dim == 128 ? launch(prompt_f32_kernel<128>, 512, 64, a, s) : launch(prompt_f32_kernel<64>, 512, 64, a, s);
   } else {
-    rc = p.head_dim == 128 ? launch_bf16<128>(ctx, a, s) : launch_bf16<64>(ctx, a, s);
+    rc = p.head_dim == 128 ? launch_bf16<128>(a, s) : launch_bf16<64>(a, s);
   }
   if (prev != ctx->device) (void)hipSetDevice(prev);
   return rc;
