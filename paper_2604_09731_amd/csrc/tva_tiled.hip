@@ -1,5 +1,5 @@
 // tree_verify_attention, tiled matrix-core path for what the interleaved-cache bf16 path does not cover: fp32 and
-// bf16, both cache layouts, head dims 64 and 128, any block size, fp8 caches.
+// bf16, both cache layouts, head dims 64 and 128, any block size, fp8 and 4-bit caches.
 //
 // The prefix is a dense contraction of all rows of a kv head (tree nodes x query heads of the group) with the cached
 // keys, so a workgroup takes a row group of up to 128 rows and streams the keys past it: every K/V byte leaves HBM once
@@ -20,7 +20,10 @@
 //     free of bank conflicts.  Interleaved pages are staged in operand order.
 //   * Nothing is rounded below what the general kernel holds: bf16 products are exact in binary32, a probability goes
 //     into the second product as the sum of three bf16 values, which is its binary32 value exactly (three MFMAs per
-//     tile instead of one; the loop is bound by its loads up to about 100 rows), and fp32 uses the fp32 MFMAs.
+//     tile instead of one; the loop is bound by its loads up to about 100 rows), and fp32 uses the fp32 MFMAs.  Against a
+//     4-bit cache a bf16 call rounds its probabilities to one bf16 (Fp4Stream).
+//   * Pages of a 4-bit cache hold operands as they are: bf16 calls with head dim 128 take them straight out of the pages or
+//     convert them once for several row tiles (Fp4Stream), the others stage them as they stage interleaved pages.
 //   * The same range, too.  A probability's smaller parts are often zero or negative and make NaN of an infinite value,
 //     and probabilities above 1 (kRescaleStep) can take the product with a very large one past binary32.  So a row that
 //     comes out infinite or NaN is evaluated once more, key by key (Finish::walk).  Looking at the finished rows takes the
@@ -33,7 +36,8 @@
 // them with the tree part.  Direct: one workgroup per segment, which also does the tree part; needs no workspace.
 //
 // The tree part (a node sees only itself and its ancestors, a handful of keys chosen by a 128-bit mask) is evaluated
-// on the vector ALUs in fp32 by walking the set bits, so what other nodes hold never enters a row.
+// on the vector ALUs in fp32 by walking the set bits, so what other nodes hold never enters a row.  (Fp4Stream takes it
+// to the matrix cores beside the prefix.)
 //
 // Measured against the general kernel (whole call): bf16 plain pages, batch 16, 32 / 8 heads of 128, prefixes of
 // 1024 .. 4096, trees of 4 .. 64 nodes 12.9 ms -> 96 us (prefix kernel 86, of which 62 are the MFMAs of its fullest
@@ -96,7 +100,7 @@ struct TiledArgs {
   int64_t* plan;   // split form: units, workers, then per sequence the units and the segments before it
   int64_t block_stride, head_stride, token_stride;
   int32_t batch, total_nodes, Hq, Hkv, G, block_size, max_blocks, num_blocks;
-  int32_t segment_cost;   // units of a segment beside its steps
+  int32_t segment_cost, tree_cost;  // units of a segment beside its steps, and of 32 nodes of its tree
   bool fp8, fp4, plain;   // the cache's element type and layout, where they are no template arguments
   bool stream;            // the prefix kernel streams, and evaluates the trees of sequences with a prefix
   uint32_t block8_magic;  // token / 8 / (block_size / 8) by multiplication
@@ -120,7 +124,7 @@ template <> struct StepCost<float> { static constexpr int one = 4, two = 7, four
 // has no rows (nothing of it is read).
 struct Shape {
   int len, base, n, rows, groups, steps;
-  int cost_last;       // of a step of the last row group (the others: StepCost::four)
+  int cost_last, extra;  // units of a step of the last row group (the others: StepCost::four), of a segment beside its steps
   int64_t full, head;  // units of a full row group, of a kv head
 };
 
@@ -139,9 +143,9 @@ __device__ inline Shape shape_of(const TiledArgs& a, int len, int base, int next
   s.steps = s.groups > 0 ? (s.len + step_keys<T>() - 1) / step_keys<T>() : 0;
   const int last = s.rows - (s.groups - 1) * kGroupRows;
   s.cost_last = last <= kRowTile ? StepCost<T>::one : (last <= 2 * kRowTile ? StepCost<T>::two : StepCost<T>::four);
-  const int extra = s.steps > 0 ? a.segment_cost : 0;
-  s.full = (int64_t)s.steps * StepCost<T>::four + extra;
-  s.head = s.groups > 0 ? (s.groups - 1) * s.full + (int64_t)s.steps * s.cost_last + extra : 0;
+  s.extra = s.steps > 0 ? a.segment_cost + a.tree_cost * ((s.n + 31) >> 5) : 0;
+  s.full = (int64_t)s.steps * StepCost<T>::four + s.extra;
+  s.head = s.groups > 0 ? (s.groups - 1) * s.full + (int64_t)s.steps * s.cost_last + s.extra : 0;
   return s;
 }
 
@@ -757,11 +761,11 @@ struct Rows<float, kPlain, D> {
   }
 };
 
-// ---- a 4-bit cache and few rows: operands straight from the pages -----------------------------------------------------------
-// One wavefront's 32 rows against tiles of 32 keys, head dim 128, and against the tree's nodes.  A lane's 16-byte vectors are its operands: of K, 32 head dims
-// of one key (the queries are laid out in the same order of the contraction); of V, four head dims of eight keys, a vector of
-// keys for each of the four output tiles (tile jt holds head dims 4 m + jt).  Nothing is shared between wavefronts, so nothing
-// goes through LDS and a wavefront keeps two tiles of its own in flight.
+// ---- a 4-bit cache: operands straight from the pages ----------------------------------------------------------------------
+// One wavefront's 32 rows against tiles of 32 keys, head dim 128, and against the tree's nodes.  A lane's 16-byte vectors are
+// its operands: of K, 32 head dims of one key (the queries are laid out in the same order of the contraction); of V, four head
+// dims of eight keys, a vector of keys for each of the four output tiles (tile jt holds head dims 4 m + jt).  With one or two row
+// tiles nothing is shared between wavefronts: nothing goes through LDS, and a wavefront keeps two tiles of its own in flight.
 // A probability is rounded to bf16 for the output product, as on the interleaved bf16 path (off by 2^-9 of itself at most, a
 // quarter of what the result's own rounding may cost; a second part would take 40 of a tile's vector instructions).
 struct Fp4Stream {
@@ -960,6 +964,132 @@ struct Fp4Stream {
     tile<true>(raw[0], len - x * 32, a.c_stored, lane);
     x += stride;
     if (x < end) tile<true>(raw[1], len - x * 32, a.c_stored, lane);
+  }
+  // ---- three and four row tiles: the conversions shared through LDS ----
+  // A step's four tiles lie as the lanes take them, 16 bytes a lane: of a tile the eight operands of the scores, then the eight of the
+  // output product.  Wavefront w converts the keys of tile w % 4 (w < 4) or its values.  160 vector instructions a wavefront and tile
+  // where every wavefront converting for itself takes 260: 32 sequences of 2048 .. 4096 tokens, 32 / 8 heads, 32 nodes 99 -> 91 us, 128
+  // nodes 356 -> 320, 4 .. 64 nodes 117.7 -> 109.2.  The barrier of every step and the first conversions cost more than that in a short
+  // piece: 4 sequences, 20 nodes, 35.0 us without, 37.5 with all pieces so, 36.3 with those of five steps and more.  Two row tiles: 59.6
+  // without, 69.1.  (What is left: a wavefront's own chain of scores, exponentials and output product; two of them on a SIMD leave
+  // its vector unit busy half of the time and its matrix core a third.)
+  static constexpr int kTileVectors = 16 * kWave, kShareSteps = 5;
+  __device__ static void read_operands(uintx4 (&x)[8], const uintx4* at, int lane) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = at[i * kWave + lane];
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  // `k`: this tile's, which become those of the tile at `next` (read in any case).
+  __device__ void tile_shared(uintx4 (&k)[8], const uintx4* at, const uintx4* next, int n_valid, float c, int lane) {
+    const int h = lane >> 5;
+    floatx16 s = (floatx16)(0.f);
+#pragma unroll
+    for (int x = 0; x < 8; ++x) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, k[x]), q[x], s, 0, 0, 0);
+    uintx4 v[8];
+    read_operands(v, at + 8 * kWave, lane);
+    if (n_valid < 32) {
+      const int left = n_valid - 8 * h;
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (16 * (i >> 3) + (i & 7) >= left) s[i] = -INFINITY;
+    }
+    bf16x8 pb[2];
+    softmax(pb, s, c);
+    if (next) read_operands(k, next, lane);
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+      for (int jt = 0; jt < D / 32; ++jt)
+        o[jt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v[4 * kk + jt]), pb[kk], o[jt], 0, 0, 0);
+  }
+  template <typename Between>
+  __device__ void run_shared(const TiledArgs& a, const int32_t* table, int g, int t0, int t1, int len, int first, bool busy,
+                             uintx4* lds, int wv, int lane, Between between) {
+    static_assert(kTilesPerStep == 4 && kWaves == 8, "a tile's keys or values a wavefront");
+    if (t0 >= t1) {
+      if (busy) between();
+      return;
+    }
+    const uint8_t* kc = (const uint8_t*)a.k_cache + (int64_t)g * a.head_stride;
+    const uint8_t* vc = (const uint8_t*)a.v_cache + (int64_t)g * a.head_stride;
+    const bool values = wv >= 4;
+    const int mine = wv & 3, h = lane >> 5, bs = a.block_size, last = (len - 1) >> 3, in8 = sigma(lane & 15) & 7;
+    int32_t id[2], slot8[2];
+    uintx4 raw[2];
+    uint64_t scale[2];
+    auto request_ids = [&](int t) {  // (past the end: the last step's once more)
+      const int at = (min(t, t1 - 1) * 4 + mine) * 4;
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk) load_id(id[kk], slot8[kk], a, table, min(at + (values ? 2 * kk + h : group_of_k(lane)), last));
+    };
+    auto request = [&]() {
+      if (values) {
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk) {
+          const uint8_t* vp = page_of(a, vc, id[kk]);
+          raw[kk] = *(const uintx4*)(vp + (uint32_t)(slot8[kk] * (4 * D) + 16 * (lane & 31)));
+          scale[kk] = *(const uint64_t*)(vp + (uint32_t)(slot8[kk] * 8 + bs * (D / 2) + ((lane & 31) >> 3) * bs));
+        }
+      } else {
+        const uint8_t* kp = page_of(a, kc, id[0]);
+        const uint32_t k_at = (uint32_t)(slot8[0] * 128 + (h * bs + in8) * 16);
+        raw[0] = *(const uintx4*)(kp + k_at);
+        raw[1] = *(const uintx4*)(kp + (k_at + 32u * bs));
+        scale[0] = *(const uint32_t*)(kp + (uint32_t)(slot8[0] * 32 + bs * (D / 2) + in8 * 4));
+      }
+    };
+    auto convert = [&](int t) {
+      uintx4* at = lds + ((t & 1) * 4 + mine) * kTileVectors + lane;
+      if (values) {
+        const int left = len - (t * 4 + mine) * 32 - 8 * h;
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk) {
+          if (left - 16 * kk < 8) keep_tokens(raw[kk], scale[kk], left - 16 * kk);
+          bf16x8 v[4];
+          bf16_of_values(v, raw[kk], scale[kk]);
+#pragma unroll
+          for (int jt = 0; jt < 4; ++jt) at[(8 + 4 * kk + jt) * kWave] = __builtin_bit_cast(uintx4, v[jt]);
+        }
+      } else {
+        const uint32_t ks = (uint32_t)scale[0] >> (8 * h);
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          const float sc = x == 0 ? smart::fp4_scale_of<0>(ks) : smart::fp4_scale_of<2>(ks);
+#pragma unroll
+          for (int w = 0; w < 4; ++w) at[(4 * x + w) * kWave] = __builtin_bit_cast(uintx4, bf16_of_codes(raw[x][w], sc));
+        }
+      }
+    };
+    request_ids(t0);
+    request();
+    request_ids(t0 + 1);
+    if (busy) between();
+    __syncthreads();  // the piece before is done with the LDS
+    convert(t0);
+    request();
+    request_ids(t0 + 2);
+    __syncthreads();
+    // The two wavefronts of a SIMD convert at different times.
+    auto ahead = [&](int t) {
+      if (t + 1 < t1) {
+        convert(t + 1);
+        request();
+        request_ids(t + 3);
+      }
+    };
+    for (int t = t0; t < t1; ++t) {
+      const uintx4* at = lds + ((t & 1) * 4 + first) * kTileVectors;
+      const int n_valid = len - (t * 4 + first) * 32;
+      if (!values) ahead(t);
+      uintx4 k[8];
+      if (busy && n_valid > 0) {
+        read_operands(k, at, lane);
+        tile_shared(k, at, at + 2 * kTileVectors, n_valid, a.c_stored, lane);
+      }
+      if (values) ahead(t);
+      if (busy && n_valid > 64) tile_shared(k, at + 2 * kTileVectors, nullptr, n_valid - 64, a.c_stored, lane);
+      __syncthreads();
+    }
   }
   // The state in LDS as Rows::put lays it down.
   __device__ void put(float* region, int lane) {
@@ -1230,7 +1360,7 @@ __global__ __launch_bounds__(kThreads, 2) void tva_tiled_kernel(TiledArgs a) {
   constexpr bool kStream = streams<T>(kCache, D);
   constexpr int kStepKeys = step_keys<T>();
   constexpr int kRegion = region_floats(D);
-  constexpr int kStageBytes = 2 * 2 * Stage::kStepChunks * 16, kFoldBytes = kWaves * kRegion * 4;
+  constexpr int kStageBytes = kStream ? 2 * kTilesPerStep * Fp4Stream::kTileVectors * 16 : 2 * 2 * Stage::kStepChunks * 16, kFoldBytes = kWaves * kRegion * 4;
   __shared__ uintx4 lds[(kStageBytes > kFoldBytes ? kStageBytes : kFoldBytes) / 16];
   __shared__ float s_ml[2][kGroupRows];
   __shared__ Sums s_part[kWaves];
@@ -1346,7 +1476,7 @@ __global__ __launch_bounds__(kThreads, 2) void tva_tiled_kernel(TiledArgs a) {
         const int cost = group < sh.groups - 1 ? StepCost<T>::four : sh.cost_last;
         const int64_t left = (int64_t)sh.steps * cost - off;  // units to the end of the segment's steps
         const int64_t share = u1 - u0;
-        u0 = min(u1, u0 + left + a.segment_cost);
+        u0 = min(u1, u0 + left + sh.extra);
         if (left <= 0) continue;  // (the finishing step does not count this worker)
         t0 = (int)(off / cost);
         t1 = share >= left ? sh.steps : (int)((off + share) / cost);
@@ -1377,10 +1507,13 @@ __global__ __launch_bounds__(kThreads, 2) void tva_tiled_kernel(TiledArgs a) {
         const int my_row0 = row0 + (busy ? rt * kRowTile : 0);
         st.begin(a, sh.base, g, my_row0, rows, lane);
         const bool ends = t1 == sh.steps;  // the piece that ends the segment has the tree part too
-        if (busy)
-          st.run(a, table, g, t0 * kTilesPerStep + first, min(t1 * kTilesPerStep, (len + 31) / 32), shared, len, lane, [&]() {
-            for (int tt = first; ends && tt * 32 < sh.n; tt += shared) st.tree_tile(a, g, sh.base, sh.n, my_row0, rows, tt, lane);
-          });
+        auto tree = [&]() {
+          for (int tt = first; ends && tt * 32 < sh.n; tt += shared) st.tree_tile(a, g, sh.base, sh.n, my_row0, rows, tt, lane);
+        };
+        if (r >= 3 && t1 - t0 >= Fp4Stream::kShareSteps)
+          st.run_shared(a, table, g, t0, t1, len, first, busy, lds, wv, lane, tree);
+        else if (busy)
+          st.run(a, table, g, t0 * kTilesPerStep + first, min(t1 * kTilesPerStep, (len + 31) / 32), shared, len, lane, tree);
         __syncthreads();  // the piece before is done with the LDS
         st.put(regions + wv * kRegion, lane);
       } else {
@@ -1733,6 +1866,10 @@ int32_t tva_launch_tiled(smart_ctx* ctx, hipStream_t stream, const tva_params& p
   a.max_blocks = p.max_blocks_per_seq;
   a.num_blocks = p.num_blocks;
   a.segment_cost = segment_cost(p, tiled_workgroups(ctx));
+  a.tree_cost = 0;
+  // Of the streaming form: 6 us to begin and fold a piece and 2 .. 4 for 32 nodes of the tree, where a step of four row tiles takes 2.4
+  // (stamps).  With 8 and 0 / these: the 4 .. 64 nodes above 115.4 / 111.9 us, 4 .. 7 nodes 44.1 / 39.7, 12 nodes 61.7 / 57.9.
+  if (stream4 && a.segment_cost > 0) a.segment_cost = 20, a.tree_cost = 8;
   a.fp8 = fp8;
   a.fp4 = fp4;
   a.stream = stream4;

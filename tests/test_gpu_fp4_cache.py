@@ -213,6 +213,27 @@ def test_attention_cut_into_other_shares(lib, oracle_attention, workers):
     _check(out, lse, ref, ref_lse, "bf16")
 
 
+@pytest.mark.parametrize("workers,bs,heads", [(1, 16, (8, 2)), (9, 64, (8, 2)), (0, 24, (4, 1)), (5, 8, (7, 1)), (2, 16, (8, 1))])
+def test_attention_of_many_rows_over_long_prefixes(lib, oracle_attention, workers, bs, heads):
+    """Three and four row tiles of 32 rows over pieces of five and more steps of 128 keys, between pieces of fewer rows or steps."""
+    import torch
+    w = W.Workload("fp4", "bf16", 7, heads[0], heads[1], 128, 0, 0, seed=31)
+    cu, parent = _trees([18, 3, 25, 32, 60, 128, 1])
+    lens = np.array([900, 1030, 1337, 129, 641, 1500, 700], np.int32)
+    call, scale, ref_args = _attend(lib, w, _case(w, cu, parent, lens, bs, 45), cu, parent, lens, bs)
+    ref, ref_lse = oracle_attention.tree_attention(*ref_args, scale)
+    lib.set_option(B.SMART_OPT_TVA_WORKERS, workers)
+    try:
+        out, lse = call()
+        _check(out, lse, ref, ref_lse, "bf16")
+        again = call()
+    finally:
+        lib.set_option(B.SMART_OPT_TVA_WORKERS, 0)
+    assert torch.equal(out, again[0]) and torch.equal(lse, again[1])
+    out, lse = call(static=True, h_cu_nodes=cu, out=torch.empty_like(out), lse=torch.empty_like(lse))
+    _check(out, lse, ref, ref_lse, "bf16")
+
+
 def test_attention_on_a_cache_with_NaN_blocks_and_bad_table_entries(lib, oracle_attention):
     """A NaN key block makes its sequence's rows NaN, and nobody else's; a table entry outside the cache is reported."""
     import torch
