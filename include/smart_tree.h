@@ -560,7 +560,8 @@ int32_t kv_cache_write_fp8(smart_ctx* ctx, void* stream, int32_t src_dtype, int3
  * dst_dtype; every value is exact in both types) is the row of slot
  * d_slot_mapping[t]; rows of negative slots and of slots outside the cache
  * become zero.
- * A slot that one writing call names twice holds afterwards any mix of the rows.
+ * A slot that one writing call names twice holds afterwards any mix of the rows'
+ * codes and scales.
  * Errors: SMART_EINVAL (null pointers, sizes, dtype; caches, strides, sources
  * and destinations that are not aligned to 16 bytes; strides smaller than a
  * page).
@@ -826,7 +827,8 @@ int32_t tree_commit_fp4(smart_ctx* ctx, void* stream, int32_t src_dtype,
  * [total_tokens][num_q_heads].  Rows of no prompt (before d_cu_tokens[0], behind
  * d_cu_tokens[batch]) are neither read nor written.  d_cu_tokens must be a running
  * sum inside [0, total_tokens]; if it is not (checked on the device), no row is
- * written.  Uses no workspace: it may be captured, and calls may overlap.
+ * written.  out and lse overlap neither each other nor the inputs.  Uses no
+ * workspace: it may be captured, and calls may run at the same time.
  * Host errors: SMART_EINVAL for null pointers, Hq % Hkv != 0, head_dim not in
  * {64, 128}, unknown dtype, softmax_scale not positive or not below 1e30,
  * total_tokens x Hq >= 2^31, token strides smaller than a token's row, k_stride or

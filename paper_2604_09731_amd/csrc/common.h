@@ -89,8 +89,8 @@ struct TvaWorkspace {
   size_t plan_bytes;
 };
 
-// Whether the pages of a 4-bit cache lie as its kernels need them: whole pages that do not overlap, every 16-byte vector
-// aligned.  (Null pointers are looked at elsewhere.)
+// Whether the pages of a 4-bit cache lie as its kernels need them: strides of a page at least, every 16-byte vector aligned.
+// (Null pointers are looked at elsewhere.)
 inline bool fp4_cache_ok(int64_t block_size, int64_t head_dim, const void* k_cache, const void* v_cache, int64_t block_stride,
                          int64_t head_stride) {
   return block_size % 8 == 0 && head_dim % 32 == 0 && head_stride >= SMART_FP4_PAGE_BYTES(block_size, head_dim) &&

@@ -1,8 +1,9 @@
 // The binding's calls in native code: output allocation, argument marshalling and the library call of the device entry
 // points, for binding.py.  A small call waits for the host, not for the GPU (a draft layer's kernel takes 4.8 us, the call took
 // 7.5 us of host time, of which the launch is 3.3): each output tensor made and each address passed from Python costs 0.1 ..
-// 1.4 us there.  No arithmetic and no checks beyond those the Python side made; the entry points come as addresses, so that
-// this module works with whichever build of the library the binding loaded.
+// 1.4 us there.  No arithmetic; the calls on 4-bit caches and prompt_attention check their tensors' shapes, types, strides and
+// devices here, the others nothing beyond what the Python side checked.  The entry points come as addresses, so that this module
+// works with whichever build of the library the binding loaded.
 #include <Python.h>
 
 #include <ATen/ATen.h>

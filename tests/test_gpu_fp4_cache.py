@@ -296,6 +296,70 @@ def test_capacity_rows_and_empty_batches(lib):
     assert none.shape[0] == 0
 
 
+@pytest.mark.parametrize("dtype,D,sizes,stride", [("bf16", 128, [3, 30], 1 << 29), ("f32", 64, [3, 30], 1 << 29), ("bf16", 128, [2, 3], 1 << 32)])
+def test_pages_far_apart(lib, oracle_attention, dtype, D, sizes, stride):
+    """Offsets past 32 bits: the blocks of a cache 2^29 bytes apart, and 2^32 (which the general kernel serves)."""
+    import torch
+    w = W.Workload("fp4", dtype, 2, 8, 2, D, 0, 0, seed=31)
+    cu, parent = _trees(sizes)
+    lens = np.array([[700, 90], [40, 3]][stride > 1 << 29], np.int32)
+    bs = 64 if stride == 1 << 29 else 16
+    args, kc, vc, table, ref_args = _case(w, cu, parent, lens, bs, 46)
+    nb, heads, page = kc.shape
+    store = torch.empty((nb - 1) * stride + 2 * heads * page, dtype=torch.uint8, device="cuda")
+    far = [store.as_strided(kc.shape, (stride, page, 1), o) for o in (0, heads * page)]
+    assert store.numel() > 1 << 32
+    slots = _dev(np.arange(nb * bs).astype(np.int64))
+    rows = lib.kv_cache_read_fp4(slots, kc, vc, D, bs, torch.float32)
+    lib.kv_cache_write_fp4(*rows, slots, *far, bs)                    # (values of the format come out as they are)
+    again = lib.kv_cache_read_fp4(slots, *far, D, bs, torch.float32)
+    for a, b in zip(rows, again):
+        assert torch.equal(a.view(torch.int32).masked_fill(a.isnan(), 0), b.view(torch.int32).masked_fill(b.isnan(), 0))
+        assert torch.equal(a.isnan(), b.isnan())
+    call, scale, _ = _attend(lib, w, (args, far[0], far[1], table, ref_args), cu, parent, lens, bs)
+    ref, ref_lse = oracle_attention.tree_attention(*ref_args, scale)
+    _check(*call(), ref, ref_lse, dtype)
+
+
+def test_a_slot_named_twice(lib):
+    """Holds codes and scales of the rows that named it; nothing else changes."""
+    import torch
+    bs, D = 8, 64
+    k, _ = _rows(3, 1, D, "bf16", 11)
+    v, _ = _rows(3, 1, D, "bf16", 12)
+    kc, vc = (torch.full((2, 1, F.page_bytes(bs, D)), 0x77, dtype=torch.uint8, device="cuda") for _ in range(2))
+    lib.kv_cache_write_fp4(k, v, _dev(np.array([9, 3, 9], np.int64)), kc, vc, bs)
+    for c, i in ((kc, 0), (vc, 1)):
+        alone = []
+        for t in (0, 2):
+            one = [torch.full_like(kc, 0x77) for _ in range(2)]
+            lib.kv_cache_write_fp4(k[1:], v[1:], _dev(np.array([3, -1], np.int64)), *one, bs)
+            lib.kv_cache_write_fp4(k[t:t + 1], v[t:t + 1], _dev(np.array([9], np.int64)), *one, bs)
+            alone.append(one[i])
+        assert ((c == alone[0]) | (c == alone[1])).all()
+
+
+def test_calls_on_two_streams_at_once():
+    import torch
+    libs = B.SmartTree(0), B.SmartTree(0)                             # a workspace each
+    w = W.Workload("fp4", "bf16", 5, 8, 2, 128, 0, 0, seed=31)
+    cu, parent = _trees([1, 6, 33, 20, 12])
+    lens = np.array([900, 2060, 1111, 1333, 65], np.int32)
+    calls = [_attend(lib, w, _case(w, cu, parent, lens, 16, 47 + i), cu, parent, lens, 16)[0] for i, lib in enumerate(libs)]
+    want = [c() for c in calls]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in calls]
+    for _ in range(3):
+        got = []
+        for c, s in zip(calls, streams):
+            with torch.cuda.stream(s):
+                got.append([c() for _ in range(4)])
+        torch.cuda.synchronize()
+        for a, b in zip(got, want):
+            for x in a:
+                assert torch.equal(x[0], b[0]) and torch.equal(x[1], b[1])
+
+
 @pytest.mark.parametrize("dtype,D,bs", [("bf16", 128, 16), ("f32", 64, 24)])
 def test_commit(lib, dtype, D, bs):
     import torch

@@ -282,3 +282,15 @@ def test_rows_far_apart(lib, dtype):
     assert torch.equal(out, near[0]) and torch.equal(lse, near[1])
     with pytest.raises(B.SmartError):
         lib.prompt_attention(q[:2], store.as_strided((2, 1, D), (1 << 24, D, 1)), v[:2], torch.tensor([0, 2], dtype=torch.int32).cuda(), 1.0)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_thousands_of_prompts(lib, dtype):
+    """Most of them empty or of one token (whose row is its value)."""
+    import torch
+    lens = np.random.default_rng(5).integers(0, 3, 5000)
+    lens[[17, 4000]] = 70, 150
+    cu = np.concatenate([[0], np.cumsum(lens)]).astype(np.int32)
+    q, k, v = _inputs(int(cu[-1]), 4, 2, 64, dtype, 10)
+    out, lse = lib.prompt_attention(q, k, v, torch.from_numpy(cu).cuda(), 0.125, want_lse=True)
+    _check(out, lse, q, k, v, cu, 0.125, dtype)
