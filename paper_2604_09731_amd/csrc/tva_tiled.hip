@@ -103,6 +103,7 @@ struct TiledArgs {
   int32_t segment_cost, tree_cost;  // units of a segment beside its steps, and of 32 nodes of its tree
   bool fp8, fp4, plain;   // the cache's element type and layout, where they are no template arguments
   bool stream;            // the prefix kernel streams, and evaluates the trees of sequences with a prefix
+  bool spread;            // direct form: consecutive segments go to different L2s
   uint32_t block8_magic;  // token / 8 / (block_size / 8) by multiplication
   float scale;
   float c;         // softmax scale in powers of two (log2 e folded in)
@@ -1367,7 +1368,7 @@ __global__ __launch_bounds__(kThreads, 2) void tva_tiled_kernel(TiledArgs a) {
   const int tid = threadIdx.x, lane = tid & (kWave - 1);
   const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
   // consecutive workers (the row groups of a segment, the two ends of one) sit behind one L2
-  const int64_t wg = gridDim.x % 8 == 0 ? (int64_t)(blockIdx.x % 8) * (gridDim.x / 8) + blockIdx.x / 8 : (int64_t)blockIdx.x;
+  const int64_t wg = gridDim.x % 8 == 0 && !(kDirect && a.spread) ? (int64_t)(blockIdx.x % 8) * (gridDim.x / 8) + blockIdx.x / 8 : (int64_t)blockIdx.x;
 
   if (kDirect && a.status)
     for (int b = (int)(wg * kWaves + wv); b < a.batch; b += gridDim.x * kWaves)
@@ -1815,18 +1816,28 @@ int32_t tva_launch_tiled(smart_ctx* ctx, hipStream_t stream, const tva_params& p
   // token, 16-node trees, 14.7 .. 15.5 us in fp32 where the general kernel takes 12.8 .. 13.8; from 8 tokens on it is behind.
   const int64_t longest = (int64_t)p.max_blocks_per_seq * p.block_size;
   const int64_t step = f32 ? step_keys<float>() : step_keys<__bf16>(), rows = (int64_t)p.total_nodes * G;
-  // Where the operands stream from 4-bit pages a step is cheaper, and a workgroup takes as long as its keys times its rows
-  // (up to 32 of them cost the same).  32 / 8 heads of 128, split and direct: one sequence, 8 nodes (32 rows), 517 tokens
-  // 16.7 / 12.1 us, 1500 17.6 / 16.0, 2050 19.5 / 18.7, 3000 21.1 / 22.5; 16 nodes, 800 tokens 18.1 / 16.8, 1030 18.9 / 19.2; 32
-  // nodes, 260 tokens 18.7 / 16.3, 517 19.9 / 20.7.  8 sequences: 2050 20.3 / 19.0, 1030 25.5 / 19.5, 517 29.3 / 21.3.  30: 8 nodes
-  // 1030 29.2 / 28.6, 2050 34.3 / 37.6, single tokens (29 segments of 4 rows a head) 30.8 / 19.5; 16 nodes 1030 37.4 / 38.1; 32 nodes 517
-  // 45.4 / 41.9.
+  // `segs` is what any offsets can make; trees much alike make `likely` (where the grid is larger, the surplus comes last: then
+  // consecutive segments go to different L2s, or those of one L2 would have them all.  30 sequences, 8 kv heads, 8 nodes, 64 tokens 18.0
+  // -> 9.9 us.)
+  // Where the operands stream from 4-bit pages a workgroup takes as long as its keys times its row tiles (1, 2, or 4 for three and
+  // four), 4.4 ns each, and the split form 9 us more than its share of all keys; of lengths that differ as 1 .. 2 do the longest is
+  // spent on all: direct up to 2048 / (1 - 0.8 likely / compute units) keys of one row tile.  32 / 8 heads of 128, equal lengths, split and
+  // direct: one sequence, 8 nodes (32 rows), 1500 tokens 17.9 / 15.7 us, 2050 18.5 / 18.5, 3000 20.4 / 22.3; 16 nodes, 800 18.1 / 16.5, 1030
+  // 18.9 / 18.9; 32 nodes, 260 20.7 / 16.0, 517 21.3 / 20.7, 800 22.6 / 24.6.  16 sequences: 8 nodes, 3000 25.4 / 23.2, 4100 28.7 / 28.1;
+  // 16 nodes, 1500 28.4 / 23.7, 3000 35.3 / 36.1; 32 nodes, 1030 35.8 / 32.0, 2050 43.5 / 50.0.  32
+  // sequences: 8 nodes, 517 21.5 / 12.7, 4100 38.9 / 31.9; 16 nodes, 517 26.3 / 16.2, 4100 59.6 / 49.3; lengths of 2048 .. 4096, 4 .. 7 nodes
+  // 38.6 / 28.7; of 512 .. 4096, 7 .. 14 nodes 50.9 / 45.4.  (A batch with a few trees of more than 128 rows among small ones has more
+  // segments than likely, and the last ones wait for a compute unit.  Row tiles of trees a quarter above the mean: 1 .. 30 nodes, 2048 ..
+  // 4096 tokens, 71 / 81.)
   const bool stream4 = fp4 && !f32 && streams<__bf16>(kE2M1, p.head_dim);
-  const int64_t mean_rows = (rows + p.batch - 1) / p.batch;
+  const int64_t cus = ctx->num_cus > 0 ? ctx->num_cus : 256, mean_rows = (rows + p.batch - 1) / p.batch;
+  const int64_t likely = (int64_t)p.batch * p.num_kv_heads * ((mean_rows + kGroupRows - 1) / kGroupRows);
+  const int64_t larger = mean_rows + mean_rows / 4, tiles = larger <= kRowTile ? 1 : (larger <= 2 * kRowTile ? 2 : 4);
+  const bool fits = segs <= cus, fits4 = fits || (likely <= cus && mean_rows <= 2 * kRowTile);
   const bool few_steps = (longest <= step && rows <= 384 * (int64_t)p.batch) ||
-                         (!f32 && longest <= 4 * step && rows <= 64 * (int64_t)p.batch) ||
-                         (stream4 && longest * (mean_rows > 32 ? mean_rows : 32) <= 65536);
-  bool direct = fixed != nullptr || (few_steps && segs <= (ctx->num_cus > 0 ? ctx->num_cus : 256));
+                         (!f32 && longest <= 4 * step && rows <= 64 * (int64_t)p.batch);
+  const bool few_steps4 = stream4 && longest * tiles * (5 * cus - 4 * (likely < cus ? likely : cus)) <= 2048 * 5 * cus;
+  bool direct = fixed != nullptr || (few_steps && fits) || (few_steps4 && fits4);
   if (!direct) {
     hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
     if (stream != nullptr && hipStreamIsCapturing(stream, &capture) != hipSuccess) (void)hipGetLastError();
@@ -1868,11 +1879,14 @@ int32_t tva_launch_tiled(smart_ctx* ctx, hipStream_t stream, const tva_params& p
   a.segment_cost = segment_cost(p, tiled_workgroups(ctx));
   a.tree_cost = 0;
   // Of the streaming form: 6 us to begin and fold a piece and 2 .. 4 for 32 nodes of the tree, where a step of four row tiles takes 2.4
-  // (stamps).  With 8 and 0 / these: the 4 .. 64 nodes above 115.4 / 111.9 us, 4 .. 7 nodes 44.1 / 39.7, 12 nodes 61.7 / 57.9.
-  if (stream4 && a.segment_cost > 0) a.segment_cost = 20, a.tree_cost = 8;
+  // (stamps); also where the segments are few.  As above with 0 for the trees / these: the 4 .. 64 nodes 115.4 / 109.0 us, 4 .. 7 nodes
+  // 44.1 / 38.5, 4 sequences of 2048 .. 4096 with 12 nodes 31.5 / 25.4, with 64 48.6 / 42.7.  14 .. 36 and 4 .. 14 in their place differ by
+  // 2 % on average.
+  if (stream4) a.segment_cost = 20, a.tree_cost = 8;
   a.fp8 = fp8;
   a.fp4 = fp4;
   a.stream = stream4;
+  a.spread = !fits && likely <= cus;
   a.plain = p.kv_layout == SMART_KV_PLAIN;
   // t8 / d as the high word of 2 t8 * (floor(2^31 / d) + 1): exact for t8 < 2^28 and d <= 8
   a.block8_magic = (uint32_t)((1ull << 31) / ((uint32_t)p.block_size / 8)) + 1u;

@@ -234,6 +234,21 @@ def test_attention_of_many_rows_over_long_prefixes(lib, oracle_attention, worker
     _check(out, lse, ref, ref_lse, "bf16")
 
 
+@pytest.mark.parametrize("sizes", [[8] * 30, [2] * 29 + [128], [0, 3] * 15 + [9]])
+def test_one_workgroup_a_segment_with_more_workgroups_than_compute_units(lib, oracle_attention, sizes):
+    """30 sequences of 8 kv heads: the launch allows for more segments than there are; trees of one to four row groups."""
+    import torch
+    w = W.Workload("fp4", "bf16", len(sizes), 32, 8, 128, 0, 0, seed=31)
+    cu, parent = _trees(sizes)
+    lens = np.random.default_rng(3).integers(0, 200, len(sizes)).astype(np.int32)
+    call, scale, ref_args = _attend(lib, w, _case(w, cu, parent, lens, 16, 49), cu, parent, lens, 16)
+    ref, ref_lse = oracle_attention.tree_attention(*ref_args, scale)
+    out, lse = call()
+    _check(out, lse, ref, ref_lse, "bf16")
+    again, again_lse = call(static=True, out=torch.empty_like(out), lse=torch.empty_like(lse))
+    _check(again, again_lse, ref, ref_lse, "bf16")
+
+
 def test_attention_on_a_cache_with_NaN_blocks_and_bad_table_entries(lib, oracle_attention):
     """A NaN key block makes its sequence's rows NaN, and nobody else's; a table entry outside the cache is reported."""
     import torch
