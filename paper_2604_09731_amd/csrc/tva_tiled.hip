@@ -1819,7 +1819,7 @@ int32_t tva_launch_tiled(smart_ctx* ctx, hipStream_t stream, const tva_params& p
   // `segs` is what any offsets can make; trees much alike make `likely` (where the grid is larger, the surplus comes last: then
   // consecutive segments go to different L2s, or those of one L2 would have them all.  30 sequences, 8 kv heads, 8 nodes, 64 tokens 18.0
   // -> 9.9 us.)
-  // Where the operands stream from 4-bit pages a workgroup takes as long as its keys times its row tiles (1, 2, or 4 for three and
+  // With a 4-bit cache and bf16.  Where the operands stream from the pages a workgroup takes as long as its keys times its row tiles (1, 2, or 4 for three and
   // four), 4.4 ns each, and the split form 9 us more than its share of all keys; of lengths that differ as 1 .. 2 do the longest is
   // spent on all: direct up to 2048 / (1 - 0.8 likely / compute units) keys of one row tile.  32 / 8 heads of 128, equal lengths, split and
   // direct: one sequence, 8 nodes (32 rows), 1500 tokens 17.9 / 15.7 us, 2050 18.5 / 18.5, 3000 20.4 / 22.3; 16 nodes, 800 18.1 / 16.5, 1030
@@ -1828,7 +1828,8 @@ int32_t tva_launch_tiled(smart_ctx* ctx, hipStream_t stream, const tva_params& p
   // sequences: 8 nodes, 517 21.5 / 12.7, 4100 38.9 / 31.9; 16 nodes, 517 26.3 / 16.2, 4100 59.6 / 49.3; lengths of 2048 .. 4096, 4 .. 7 nodes
   // 38.6 / 28.7; of 512 .. 4096, 7 .. 14 nodes 50.9 / 45.4.  (A batch with a few trees of more than 128 rows among small ones has more
   // segments than likely, and the last ones wait for a compute unit.  Row tiles of trees a quarter above the mean: 1 .. 30 nodes, 2048 ..
-  // 4096 tokens, 71 / 81.)
+  // 4096 tokens, 71 / 81.)  Head dim 64, whose steps take 8.4 ns a key and whose split form 4 us, counts as four tiles: 8 nodes, one
+  // sequence, 517 tokens 13.9 / 13.2, 1030 14.2 / 17.5; 32 sequences, 130 15.5 / 10.4, 1030 24.4 / 18.6, 4100 54.2 / 49.5.
   const bool stream4 = fp4 && !f32 && streams<__bf16>(kE2M1, p.head_dim);
   const int64_t cus = ctx->num_cus > 0 ? ctx->num_cus : 256, mean_rows = (rows + p.batch - 1) / p.batch;
   const int64_t likely = (int64_t)p.batch * p.num_kv_heads * ((mean_rows + kGroupRows - 1) / kGroupRows);
@@ -1836,7 +1837,7 @@ int32_t tva_launch_tiled(smart_ctx* ctx, hipStream_t stream, const tva_params& p
   const bool fits = segs <= cus, fits4 = fits || (likely <= cus && mean_rows <= 2 * kRowTile);
   const bool few_steps = (longest <= step && rows <= 384 * (int64_t)p.batch) ||
                          (!f32 && longest <= 4 * step && rows <= 64 * (int64_t)p.batch);
-  const bool few_steps4 = stream4 && longest * tiles * (5 * cus - 4 * (likely < cus ? likely : cus)) <= 2048 * 5 * cus;
+  const bool few_steps4 = fp4 && !f32 && longest * (stream4 ? tiles : 4) * (5 * cus - 4 * (likely < cus ? likely : cus)) <= 2048 * 5 * cus;
   bool direct = fixed != nullptr || (few_steps && fits) || (few_steps4 && fits4);
   if (!direct) {
     hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
