@@ -13,7 +13,6 @@
 #include <math.h>
 
 #include "common.h"
-#include "wave.h"
 
 namespace {
 
@@ -63,10 +62,20 @@ __device__ inline float sum_quarters(float x) {
   return sum_halves(__uint_as_float(r[0]) + __uint_as_float(r[1]));
 }
 
+// `op` over the 64 lanes, the same in all of them: lanes 1, 2, 4 and 8 apart by data-parallel moves, 16 and 32 apart by swaps.
+template <typename Op>
+__device__ inline int wave_all(int v, Op op) {
+  v = op(v, __builtin_amdgcn_update_dpp(0, v, 0xB1, 0xF, 0xF, true));   // quads: 1, 0, 3, 2
+  v = op(v, __builtin_amdgcn_update_dpp(0, v, 0x4E, 0xF, 0xF, true));   // 2, 3, 0, 1
+  v = op(v, __builtin_amdgcn_update_dpp(0, v, 0x141, 0xF, 0xF, true));  // half rows mirrored
+  v = op(v, __builtin_amdgcn_update_dpp(0, v, 0x140, 0xF, 0xF, true));  // rows mirrored
+  const auto r = __builtin_amdgcn_permlane16_swap((uint32_t)v, (uint32_t)v, false, false);
+  v = op((int)r[0], (int)r[1]);
+  const auto h = __builtin_amdgcn_permlane32_swap((uint32_t)v, (uint32_t)v, false, false);
+  return __builtin_amdgcn_readfirstlane(op((int)h[0], (int)h[1]));
+}
 __device__ inline int wave_sum(int v) {
-  int64_t total;
-  smart::wave_excl_scan(v, threadIdx.x & (kWave - 1), &total);
-  return (int)total;
+  return wave_all(v, [](int x, int y) { return x + y; });
 }
 
 // ---- which rows a workgroup takes ------------------------------------------------------------------------------------
@@ -96,8 +105,7 @@ __device__ inline Item find_item(const PromptArgs& a, int rank) {
     const int tiles = tiles_of(len);
     if (wave_sum(tiles) <= rank) return it;
     int lo = 0, hi = tiles;  // C(hi) <= rank < C(lo); the same in all lanes, which take part in the sums together
-    for (int o = 32; o > 0; o >>= 1) hi = max(hi, __shfl_xor(hi, o));
-    hi = __builtin_amdgcn_readfirstlane(hi);
+    hi = wave_all(hi, [](int x, int y) { return max(x, y); });
     int above = 0;  // C(hi)
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1, c = wave_sum(max(0, tiles - mid));
@@ -233,7 +241,7 @@ __device__ void walk(const PromptArgs& a, int base, int token, int head, int lan
 // reads bring: a score's step (x, e) over the head dims 16 x + 4 w + e, and row i of output tile (x, e) is head dim 64 x + 4 i + e.
 // Two wavefronts share rows and take the two halves of every stage, so that a compute unit has two on each matrix core even
 // where it has one row tile, and a long prompt's last tile, which nothing can follow, takes half as long.  8 / 2 heads of 64:
-// 6600 tokens of 8 prompts 106 us (98 TFLOP/s; with 32 x 32 tiles, 128 rows and no sharing 148; 64 rows without sharing 110), one
+// 6600 tokens of 8 prompts 103 us (102 TFLOP/s; with 32 x 32 tiles, 128 rows and no sharing 148; 64 rows without sharing 110), one
 // prompt of 1536 62 (129, 72), of 300 16.6 (29, 17.7), 4 of 4096 571 (653, 579); head dim 128, 4 of 2048 324 (335, 341).  Left without
 // the softmax it takes 6 % less, without staging 8 %; the rest is what the ends of the row tiles leave idle.
 template <int D>

@@ -164,6 +164,7 @@ _SHAPES = [
     ("bf16", 128, 16, (32, 8), [7], [517]),
     ("bf16", 128, 16, (8, 1), [1, 1, 1, 1], [2000, 1, 64, 1025]),
     ("bf16", 128, 16, (7, 1), [4, 5, 9, 10], [640, 95, 1500, 16]),
+    ("bf16", 128, 16, (8, 1), [1, 1, 2], [5000, 1, 4097]),
     ("bf16", 128, 64, (8, 2), [1, 9, 16, 20], [100, 63, 64, 700]),
     ("bf16", 128, 24, (4, 4), [1, 8, 33, 2], [100, 23, 24, 700]),
     ("bf16", 128, 8, (8, 2), [1, 8, 33, 2], [100, 7, 8, 700]),
