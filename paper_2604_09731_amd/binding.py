@@ -443,11 +443,6 @@ def _ptr(t):
     return t.data_ptr() if t is not None else None
 
 
-def _on_gpu(t):
-    if not t.is_cuda:       # (a kernel that reads host addresses faults)
-        raise ValueError(f"expected tensors on the GPU, got one on {t.device}")
-
-
 def _whole_rows(n):
     return (n + _ROW - 1) // _ROW * _ROW
 
@@ -581,16 +576,20 @@ class SmartTree:
         self._native.cache_write(self._ctx, k_src, v_src, slot_mapping, k_cache, v_cache, layout, block_size, num_blocks,
                                  block_stride, head_stride, token_stride, True, k_scale, v_scale)
 
+    def _here(self, t):     # (a kernel that reads host addresses faults; _marshal looks at the current device)
+        if t.get_device() != self.device:
+            raise ValueError(f"expected tensors on this handle's GPU, got one on {t.device}")
+
     def kv_cache_write_fp4(self, k_src, v_src, slot_mapping, k_cache, v_cache, block_size):
         """Rows [n, Hkv, D] into 4-bit caches: uint8 tensors [num_blocks, Hkv, fp4_page_bytes(block_size, D)]."""
-        _on_gpu(k_src)
+        self._here(k_src)
         self._native.cache_write_fp4(self._ctx, k_src, v_src, slot_mapping, k_cache, v_cache, block_size)
 
     def kv_cache_read_fp4(self, slot_mapping, k_cache, v_cache, head_dim, block_size, dtype=None, k_out=None, v_out=None):
         """The rows of the slots as values, (k, v) [n, Hkv, D] of ``dtype`` (default bfloat16; exact in float32 too);
         zeros for slots that are negative or outside the cache."""
         torch = _torch()
-        _on_gpu(k_cache)
+        self._here(k_cache)
         shape = (slot_mapping.shape[0], k_cache.shape[1], int(head_dim))
         k_out, v_out = (torch.empty(shape, dtype=dtype or torch.bfloat16, device=k_cache.device) if t is None else t
                         for t in (k_out, v_out))
@@ -604,7 +603,7 @@ class SmartTree:
         """Causal attention of packed prompts: q [T, Hq, D], k and v [T, Hkv, D] (tokens may be strided, as parts of one
         projection's output are), prompt b the tokens cu_tokens[b] .. cu_tokens[b + 1] - 1.  Returns out (like q,
         contiguous unless given), or (out, lse [T, Hq]) if lse is given or wanted; rows of no prompt are not written."""
-        _on_gpu(q)
+        self._here(q)
         return self._native.prompt(self._ctx, q, k, v, cu_tokens, softmax_scale, out, lse, want_lse)
 
     # -- tree_verify_attention ---------------------------------------------
@@ -626,6 +625,8 @@ class SmartTree:
             h_address = h_cu_nodes.ctypes.data
         if kv_cache_dtype not in (None, SMART_FP8_E4M3, SMART_FP4_E2M1):
             raise ValueError(f"kv_cache_dtype {kv_cache_dtype!r}")
+        if kv_cache_dtype == SMART_FP4_E2M1:
+            self._here(q)
         call = self._native.attention_fp4 if kv_cache_dtype == SMART_FP4_E2M1 else self._native.attention
         return call(self._ctx, q, k_tree, v_tree, k_cache, v_cache, block_table, prefix_len, cu_nodes,
                     anc_mask, softmax_scale, kv_layout, block_size, out, lse, want_lse, h_address, k_scale, v_scale, static,
@@ -653,6 +654,6 @@ class SmartTree:
     def tree_commit_fp4(self, cu_nodes, accept_len, accept_path, k_tree, v_tree, k_cache, v_cache, block_table, prefix_len,
                         block_size):
         """tree_commit into 4-bit caches (see kv_cache_write_fp4); returns (new_prefix_len, status)."""
-        _on_gpu(cu_nodes)
+        self._here(cu_nodes)
         return self._native.commit_fp4(self._ctx, cu_nodes, accept_len, accept_path, k_tree, v_tree, k_cache, v_cache,
                                        block_table, prefix_len, block_size)

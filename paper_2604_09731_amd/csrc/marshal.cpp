@@ -102,8 +102,14 @@ int32_t element_type(const at::Tensor& t) {
   PyErr_Format(PyExc_TypeError, "unsupported element type %s", toString(t.scalar_type()));
   throw Failed();
 }
-void* stream() {
+// The current device's stream.  `on`: a tensor that has to be on that device, if any.
+void* stream(const at::Tensor* on = nullptr) {
   PyObject* device = must(PyObject_CallNoArgs(get_device));
+  if (on && on->is_cuda() && on->get_device() != PyLong_AsLong(device)) {
+    Py_DECREF(device);
+    PyErr_SetString(PyExc_ValueError, "tensors on another device than the current one");
+    throw Failed();
+  }
   PyObject* s = PyObject_CallOneArg(raw_stream, device);
   Py_DECREF(device);
   must(s);
@@ -370,7 +376,7 @@ PyObject* cache_write_fp4(PyObject* const* a) {  // ctx, k_src, v_src, slots, k_
   page_bytes(kc, vc, Hkv, bs, D);
   one_device({&k, &v, &slots, &kc, &vc});
   const int32_t blocks_held = extent32(kc.size(0));
-  void* s = stream();
+  void* s = stream(&k);
   call("kv_cache_write_fp4", [&] {
     return lib.cache_write_fp4(ctx, s, type, n, Hkv, D, bs, blocks_held, address(k), address(v), address<int64_t>(slots),
                                address(kc), address(vc), kc.stride(0), kc.stride(1));
@@ -390,7 +396,7 @@ PyObject* cache_read_fp4(PyObject* const* a) {  // ctx, slots, k_cache, v_cache,
   page_bytes(kc, vc, Hkv, bs, D);
   one_device({&k, &v, &slots, &kc, &vc});
   const int32_t blocks_held = extent32(kc.size(0));
-  void* s = stream();
+  void* s = stream(&k);
   call("kv_cache_read_fp4", [&] {
     return lib.cache_read_fp4(ctx, s, type, n, Hkv, D, bs, blocks_held, address(kc), address(vc), kc.stride(0), kc.stride(1),
                               address<int64_t>(slots), address(k), address(v));
@@ -418,7 +424,7 @@ PyObject* commit_fp4(PyObject* const* a) {
   one_device({&kt, &vt, &kc, &vc, &cu, &length, &path, &table, &prefix});
   auto rows = i32_rows(2, batch, cu);
   const int32_t blocks_held = extent32(kc.size(0));
-  void* s = stream();
+  void* s = stream(&kt);
   call("tree_commit_fp4", [&] {
     return lib.commit_fp4(ctx, s, type, batch, depth, Hkv, D, bs, blocks, blocks_held, address<int32_t>(cu),
                           address<int32_t>(length), address<int32_t>(path), address(kt), address(vt), address<int32_t>(table),
@@ -476,7 +482,7 @@ PyObject* prompt(PyObject* const* a) {  // ctx, q, k, v, cu_tokens, scale, out, 
   p.d_cu_tokens = address<int32_t>(cu);
   p.d_out = address(out);
   p.d_lse = lse.defined() ? address<float>(lse) : nullptr;
-  void* s = stream();
+  void* s = stream(&q);
   call("prompt_attention", [&] { return lib.prompt(ctx, s, &p); });
   return lse.defined() ? tuple_of(out, lse) : wrap(out);
 }

@@ -5,6 +5,7 @@ import importlib.machinery
 import importlib.util
 import os
 import shutil
+import types
 
 import pytest
 import torch
@@ -170,7 +171,7 @@ def test_parts_of_a_projection_are_taken_as_they_lie(native):
 
 def test_tensors_off_the_gpu_are_refused():
     lib = object.__new__(B.SmartTree)
-    lib._native, lib._h = None, None
+    lib._native, lib._h, lib.device = None, None, 0
     with pytest.raises(ValueError):
         lib.prompt_attention(Q, KV, KV, CU, 0.1)
     with pytest.raises(ValueError):
@@ -181,3 +182,15 @@ def test_tensors_off_the_gpu_are_refused():
         lib.tree_commit_fp4(CU, I32, I32, KV, KV, CACHE, CACHE, I32, I32, 16)
     with pytest.raises(ValueError):
         lib.tree_verify_attention(Q, KV, KV, CACHE, CACHE, I32, I32, CU, SLOTS, 0.1, 1, kv_cache_dtype=7)
+    with pytest.raises(ValueError):
+        lib.tree_verify_attention(Q, KV, KV, CACHE, CACHE, I32, I32, CU, SLOTS, 0.1, 1, kv_cache_dtype=B.SMART_FP4_E2M1)
+
+
+def test_tensors_on_another_gpu_are_refused():
+    lib = object.__new__(B.SmartTree)
+    lib._native, lib._h, lib.device = None, None, 0
+    there = types.SimpleNamespace(get_device=lambda: 1, device=torch.device("cuda", 1), shape=(9, 8, 64))
+    for call in (lambda: lib.prompt_attention(there, KV, KV, CU, 0.1), lambda: lib.kv_cache_write_fp4(there, KV, SLOTS, CACHE, CACHE, 16),
+                 lambda: lib.kv_cache_read_fp4(SLOTS, there, CACHE, 64, 16)):
+        with pytest.raises(ValueError):
+            call()
