@@ -1003,14 +1003,12 @@ struct Fp4Stream {
       for (int jt = 0; jt < D / 32; ++jt)
         o[jt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v[4 * kk + jt]), pb[kk], o[jt], 0, 0, 0);
   }
+  // Steps t0 .. t1 - 1, at least one; all wavefronts of the workgroup together, of which the `busy` ones have rows.  A step is
+  // requested two steps and converted one step ahead.
   template <typename Between>
   __device__ void run_shared(const TiledArgs& a, const int32_t* table, int g, int t0, int t1, int len, int first, bool busy,
                              uintx4* lds, int wv, int lane, Between between) {
     static_assert(kTilesPerStep == 4 && kWaves == 8, "a tile's keys or values a wavefront");
-    if (t0 >= t1) {
-      if (busy) between();
-      return;
-    }
     const uint8_t* kc = (const uint8_t*)a.k_cache + (int64_t)g * a.head_stride;
     const uint8_t* vc = (const uint8_t*)a.v_cache + (int64_t)g * a.head_stride;
     const bool values = wv >= 4;
