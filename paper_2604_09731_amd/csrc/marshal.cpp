@@ -487,6 +487,46 @@ PyObject* prompt(PyObject* const* a) {  // ctx, q, k, v, cu_tokens, scale, out, 
   return lse.defined() ? tuple_of(out, lse) : wrap(out);
 }
 
+// A tensor argument that may be None.
+const at::Tensor* optional(PyObject* o) { return o == Py_None ? nullptr : &tensor(o); }
+
+// What attention over a 4-bit cache needs of its tensors beside the caches' pages (page_bytes), for the arguments below.
+void attention_tensors(PyObject* const* a) {
+  const at::Tensor &q = tensor(a[1]), &kt = tensor(a[2]), &vt = tensor(a[3]), &length = tensor(a[7]), &cu = tensor(a[8]), &mask = tensor(a[9]);
+  three_dims(kt);
+  same_shape(kt, vt, "k_tree and v_tree");
+  for (const at::Tensor* t : {&q, &kt, &vt}) contiguous(*t, "tree_verify_attention");
+  if (kt.scalar_type() != q.scalar_type() || kt.size(0) < q.size(0) || kt.size(2) != q.size(2) || cu.dim() != 1) {
+    PyErr_SetString(PyExc_ValueError, "tree_verify_attention: q [N, Hq, D], k_tree and v_tree [N, Hkv, D] of one element type, cu_nodes [B + 1]");
+    throw Failed();
+  }
+  const int64_t batch = cu.size(0) - 1;
+  elements(cu, at::kInt, 1, "cu_nodes");
+  elements(length, at::kInt, batch, "prefix_len");
+  elements(mask, at::kLong, 2 * q.size(0), "anc_mask");
+  one_device({&q, &kt, &vt, &length, &cu, &mask});
+  if (const at::Tensor* kc = optional(a[4])) {
+    const at::Tensor &vc = tensor(a[5]), &table = tensor(a[6]);
+    elements(table, at::kInt, batch * extent(table, 1), "block_table");
+    one_device({&q, kc, &vc, &table});
+    extent32(kc->size(0));
+  }
+  if (const at::Tensor* out = optional(a[13])) {
+    same_shape(q, *out, "out");
+    contiguous(*out, "out");
+  }
+  if (const at::Tensor* lse = optional(a[14])) {
+    elements(*lse, at::kFloat, q.size(0) * q.size(1), "lse");
+    one_device({&q, lse});
+  }
+  if (const at::Tensor* status = optional(a[20])) {
+    elements(*status, at::kInt, batch, "status");
+    one_device({&q, status});
+  }
+  extent32(q.size(0));
+  extent32(batch);
+}
+
 // ctx, q, k_tree, v_tree, k_cache, v_cache, block_table, prefix_len, cu_nodes, anc_mask, scale, layout, block_size, out, lse,
 // want_lse, address of the host's offsets, k_scale, v_scale, static, status
 template <bool kFp4>
@@ -494,6 +534,7 @@ PyObject* attention_over(PyObject* const* a) {
   auto ctx = pointer<smart_ctx>(a[0]);
   const at::Tensor &q = tensor(a[1]), &kt = tensor(a[2]), &vt = tensor(a[3]), &cu = tensor(a[8]);
   three_dims(q);
+  if (kFp4) attention_tensors(a);
   at::Tensor out = a[13] == Py_None ? at::empty_like(q) : tensor(a[13]), lse;
   const bool want_lse = truth(a[15]);
   tva_params p = {};
@@ -550,7 +591,7 @@ PyObject* attention_over(PyObject* const* a) {
   p.d_lse = lse.defined() ? address<float>(lse) : nullptr;
   p.d_status = address<int32_t>(a[20]);
   p.h_cu_nodes = pointer<const int32_t>(a[16]);
-  void* s = stream();
+  void* s = kFp4 ? stream(&q) : stream();
   if (truth(a[19])) call("tree_verify_attention_static", [&] { return lib.attention_static(ctx, s, &p); });
   else call("tree_verify_attention", [&] { return lib.attention(ctx, s, &p); });
   return lse.defined() ? tuple_of(out, lse) : wrap(out);
