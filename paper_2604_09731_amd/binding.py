@@ -625,6 +625,8 @@ class SmartTree:
             h_address = h_cu_nodes.ctypes.data
         if kv_cache_dtype not in (None, SMART_FP8_E4M3, SMART_FP4_E2M1):
             raise ValueError(f"kv_cache_dtype {kv_cache_dtype!r}")
+        if kv_cache_dtype == SMART_FP8_E4M3 and k_cache is not None and k_cache.dtype != _torch().uint8:
+            raise ValueError(f"kv_cache_dtype SMART_FP8_E4M3, but the caches hold {k_cache.dtype}")
         if kv_cache_dtype == SMART_FP4_E2M1:
             self._here(q)
         call = self._native.attention_fp4 if kv_cache_dtype == SMART_FP4_E2M1 else self._native.attention

@@ -3,6 +3,7 @@ shape, layout and device is looked at before its address goes to the library."""
 import pytest
 import torch
 
+from paper_2604_09731_amd import binding as B
 from tests.test_fp4_prompt_arguments import CACHE, CALLS, CU, I32, KV, Q, native  # noqa: F401  (native: a fixture)
 
 TABLE, MASK = torch.zeros(2, 3, dtype=torch.int32), torch.zeros(9, 2, dtype=torch.int64)
@@ -41,3 +42,19 @@ def test_attention_over_a_4_bit_cache_takes_all_that_fits(native):  # noqa: F811
     args[4] = args[5] = args[6] = None                                      # no cached prefix
     module.attention_fp4(*args)
     assert called.pop()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32, torch.int8])
+def test_a_cache_said_to_hold_fp8_that_holds_something_else_is_refused(dtype):
+    called = []
+    lib = object.__new__(B.SmartTree)
+    lib._native, lib._h, lib.device = type("native", (), {"attention": lambda *a: called.append(a)}), None, 0
+    cache = torch.zeros(3, 2, 16, 64, dtype=dtype)
+    with pytest.raises(ValueError):
+        lib.tree_verify_attention(Q, KV, KV, cache, cache, TABLE, I32, CU, MASK, 0.1, B.SMART_KV_PLAIN, k_scale=1.0, v_scale=1.0,
+                                  kv_cache_dtype=B.SMART_FP8_E4M3)
+    assert not called
+    bytes_ = cache.to(torch.uint8)
+    lib.tree_verify_attention(Q, KV, KV, bytes_, bytes_, TABLE, I32, CU, MASK, 0.1, B.SMART_KV_PLAIN, k_scale=1.0, v_scale=1.0,
+                              kv_cache_dtype=B.SMART_FP8_E4M3)
+    assert len(called) == 1
