@@ -820,7 +820,8 @@ int32_t tree_commit_fp4(smart_ctx* ctx, void* stream, int32_t src_dtype,
  * rounded to bf16 before the second product and the sum that divides it is taken
  * over the rounded ones (so that equal values come out as they are); lse is that
  * of the unrounded weights.  What later tokens hold, infinities and NaN included,
- * never enters a row.
+ * never enters a row.  A score of -infinity has no weight (a row of nothing else is
+ * zero, its lse -infinity); a row with a score of NaN or +infinity is NaN, its lse too.
  * q, out [total_tokens][num_q_heads][head_dim], k, v [total_tokens][num_kv_heads]
  * [head_dim]; the four token strides count elements, so q, k and v may be parts of
  * one projection's output (heads and head dims are contiguous).  lse

@@ -436,7 +436,7 @@ __global__ __launch_bounds__(512, D == 64 ? 4 : 2) void prompt_f32_kernel(Prompt
       if (there)
         *(floatx4*)((float*)a.out + (int64_t)(base + token) * a.out_stride + (int64_t)head * D + 64 * x + 16 * w + 4 * r) = y;
     }
-  if (a.lse && there && w == 0) a.lse[(int64_t)(base + token) * a.Hq + head] = sum > 0.f ? m * a.scale + logf(sum) : -INFINITY;
+  if (a.lse && there && w == 0) a.lse[(int64_t)(base + token) * a.Hq + head] = sum == 0.f ? -INFINITY : m * a.scale + logf(sum);
   uint64_t again = __ballot(there && bad != 0.f && sum < INFINITY);
   again = (again | again >> 16 | again >> 32 | again >> 48) & 0xFFFFull;
   if (again) evaluate_again<float, D>(a, base, g, mine, rows, (uint32_t)again, lane);
@@ -611,7 +611,7 @@ struct RowsBf16 {
       }
       if (kLse) {
         const float all = sum_quarters(exact[r]);
-        if (there && w == 0) a.lse[(int64_t)(base + token[r]) * a.Hq + head] = all > 0.f ? mc[r] * kLn2 + logf(all) : -INFINITY;
+        if (there && w == 0) a.lse[(int64_t)(base + token[r]) * a.Hq + head] = all == 0.f ? -INFINITY : mc[r] * kLn2 + logf(all);
       }
       // an infinity or NaN that does not come from NaN scores (those stay NaN whichever way they are summed)
       uint64_t again = __ballot(there && bad != 0.f && sum < INFINITY);

@@ -94,3 +94,26 @@ def test_a_bad_value_of_the_first_token_costs_no_more_than_some_calls(lib, dtype
     assert (out[:, :, 7] == float("inf")).all()
     _some_rows(out, q, k, v, 0, [0, 1, 777, n - 1], [0, Hq - 1], D ** -0.5, dtype)
     assert slow <= 40 * clean
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+@pytest.mark.parametrize("at", [0, 40])
+def test_rows_with_scores_that_are_no_numbers_have_no_log_sum_exp(lib, dtype, D, bad, at):
+    """A NaN or an infinite score: the row is NaN, and its log-sum-exp too (not -infinity, which says that nothing has weight)."""
+    import torch
+    n = 150
+    q, k, v = _inputs(n, 4, 2, D, dtype, 44)
+    cu = torch.tensor([0, n], dtype=torch.int32, device="cuda")
+    clean, clean_lse = lib.prompt_attention(q, k, v, cu, D ** -0.5, want_lse=True)
+    q[..., 3] = 1.0
+    k[at, 1, 3] = bad                                   # of kv head 1: query heads 2 and 3
+    q[90, 0, 7] = float("nan")
+    out, lse = lib.prompt_attention(q, k, v, cu, D ** -0.5, want_lse=True)
+    assert out[at:, 2:].isnan().all() and lse[at:, 2:].isnan().all()
+    assert out[90, 0].isnan().all() and lse[90, 0].isnan()
+    assert torch.isfinite(out[:at]).all() and torch.isfinite(lse[:at]).all()
+    others = [t for t in range(n) if t != 90]
+    assert torch.isfinite(out[others, :2]).all() and torch.isfinite(lse[others, :2]).all()
+    assert torch.isfinite(clean).all() and torch.isfinite(clean_lse).all()
