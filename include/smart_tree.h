@@ -595,7 +595,11 @@ int32_t kv_cache_read_fp4(smart_ctx* ctx, void* stream, int32_t dst_dtype, int32
  * SMART_FP8_E4M3) the cached keys and values are k_scale / v_scale times the
  * stored E4M3 values (exact in bf16); everything else is as above.  With a 4-bit
  * cache (SMART_FP4_E2M1) they are the values that the page's codes and scales
- * stand for (exact in bf16 as well).  A tree's
+ * stand for (exact in bf16 as well), and bf16 calls round softmax weights to bf16
+ * before the second product, whatever the block size and head_dim, and divide by
+ * the sum of the rounded ones (so that equal values come out as they are); lse is
+ * that of the unrounded weights.  (Where pages lie 2^32 bytes apart or tree rows
+ * are not aligned to 16 bytes the weights stay in fp32.)  A tree's
  * rows per kv head, n x G, are served in groups of up to 256 (of 128 by the
  * tiled kernel), each of which reads the prefix once.
  *

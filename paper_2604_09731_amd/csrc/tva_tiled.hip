@@ -21,7 +21,7 @@
 //   * Nothing is rounded below what the general kernel holds: bf16 products are exact in binary32, a probability goes
 //     into the second product as the sum of three bf16 values, which is its binary32 value exactly (three MFMAs per
 //     tile instead of one; the loop is bound by its loads up to about 100 rows), and fp32 uses the fp32 MFMAs.  Against a
-//     4-bit cache a bf16 call rounds its probabilities to one bf16 (Fp4Stream).
+//     4-bit cache a bf16 call rounds its probabilities to one bf16 and divides by the sum of the rounded ones (rounds_weights).
 //   * Pages of a 4-bit cache hold operands as they are: bf16 calls with head dim 128 take them straight out of the pages or
 //     convert them once for several row tiles (Fp4Stream), the others stage them as they stage interleaved pages.
 //   * The same range, too.  A probability's smaller parts are often zero or negative and make NaN of an infinite value,
@@ -81,7 +81,8 @@ template <> struct TileKeys<__bf16> { static constexpr int value = 32; };
 template <> struct TileKeys<float> { static constexpr int value = 16; };
 template <typename T> constexpr int step_keys() { return kTilesPerStep * TileKeys<T>::value; }
 
-__host__ __device__ constexpr int slot_floats(int D) { return kGroupRows * (D + 2); }
+// Of a partial: O, the row maxima, the divisors, and (exact, see rounds_weights) the sums of unrounded weights.
+__host__ __device__ constexpr int slot_floats(int D, bool exact) { return kGroupRows * (D + (exact ? 3 : 2)); }
 
 struct TiledArgs {
   const void* q;
@@ -213,6 +214,18 @@ __device__ inline float sum_rows16(float x) {
   return sum_halves(__uint_as_float(r[0]) + __uint_as_float(r[1]));
 }
 
+// `sum` and a pair of bf16.
+__device__ inline float add_pair(uint32_t pair, float sum) {
+  return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pair), __builtin_bit_cast(bf16x2, 0x3F803F80u), sum, false);
+}
+__device__ inline float add_bf16(bf16x8 x, float sum) {
+  const uintx4 pairs = __builtin_bit_cast(uintx4, x);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) sum = add_pair(pairs[i], sum);
+  return sum;
+}
+__device__ inline float sum8(floatx8 p) { return ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7])); }
+
 // exp2((x - m) c) with an empty reference (m = -inf: no key so far scored above -inf) giving 0 for x = -inf.
 __device__ inline float weight(float x, float m, float c) {
   return __builtin_amdgcn_exp2f((x - (m == -INFINITY ? 0.f : m)) * c);
@@ -263,6 +276,16 @@ enum CacheType { kSameType, kE4M3, kE2M1 };
 template <typename T>
 constexpr bool streams(CacheType cache, int D) {
   return cache == kE2M1 && sizeof(T) == 2 && D == 128;
+}
+
+// Whether a probability enters the output product as one bf16: a 4-bit cache's values have two significant bits, and three products
+// in place of one would take most of a tile's time.  It is off by up to 2^-8 of itself then; the sum that divides is taken over
+// the rounded ones, so that a row that one key dominates comes out as that key's value and equal values as they are, and a row is
+// off by 2 2^-8 of its weighted mean |V| at most, about what rounding the result may cost (2^-8 of it).  The log-sum-exp needs the
+// sums of the unrounded ones beside them; they are carried where it is asked for (kExact).
+template <typename T>
+constexpr bool rounds_weights(CacheType cache) {
+  return cache == kE2M1 && sizeof(T) == 2;
 }
 
 template <typename T, CacheType kCache, bool kPlain, int D>
@@ -518,7 +541,8 @@ struct Rows<__bf16, kPlain, D> {
   static constexpr int kRowChunks = D / 8;
   bf16x8 q[D / 16];
   floatx16 o[D / 32];
-  float m, l;  // of row lane % 32; l: this half-wavefront's keys
+  float m, l;   // of row lane % 32; l: this half-wavefront's keys
+  float exact;  // l of unrounded weights
 
   __device__ void begin(const TiledArgs& a, int base, int g, int row0, int rows, int lane) {
     const int h = lane >> 5, j = lane & 31;
@@ -533,11 +557,11 @@ struct Rows<__bf16, kPlain, D> {
 #pragma unroll
     for (int jt = 0; jt < D / 32; ++jt) o[jt] = (floatx16)(0.f);
     m = -INFINITY;
-    l = 0.f;
+    l = exact = 0.f;
   }
   __device__ static int key_of_row(int i) { return kPlain ? i : (i & 16) + sigma(i & 15); }
 
-  template <bool kInPlace, bool kOnePart>
+  template <bool kInPlace, bool kOnePart, bool kExact>
   __device__ void tile(const uintx4* kt, const uintx4* vt, int n_valid, float c, int lane) {
     const int h = lane >> 5, j = lane & 31;
     const int key = key_of_row(j);
@@ -568,6 +592,7 @@ struct Rows<__bf16, kPlain, D> {
     if (__any((m_new - m) * c > kRescaleStep)) {
       const float alpha = weight(m, m_new, c);
       l *= alpha;
+      if (kExact) exact *= alpha;
 #pragma unroll
       for (int jt = 0; jt < D / 32; ++jt) o[jt] *= alpha;
       m = m_new;
@@ -577,10 +602,12 @@ struct Rows<__bf16, kPlain, D> {
       floatx8 p;
 #pragma unroll
       for (int e = 0; e < 8; ++e) p[e] = weight(s[8 * kk + e], m, c);
-      l += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
+      if (!kOnePart) l += sum8(p);
+      if (kExact) exact += sum8(p);
       // p = hi + mid + lo exactly: three bf16 values hold the 24 bits of a binary32
       const bf16x8 hi = __builtin_convertvector(p, bf16x8);
       if (kOnePart) {
+        l = add_bf16(hi, l);
 #pragma unroll
         for (int jt = 0; jt < D / 32; ++jt) o[jt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[kk][jt], hi, o[jt], 0, 0, 0);
         continue;
@@ -612,7 +639,8 @@ struct Rows<__bf16, kPlain, D> {
     }
     return __builtin_bit_cast(bf16x8, __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7));
   }
-  // The state in LDS: O as [d / 4][32 rows][4], the row maxima, the row sums.
+  // The state in LDS: O as [d / 4][32 rows][4], the row maxima, the row sums (of both kinds).
+  template <bool kExact>
   __device__ void put(float* region, int lane) {
     const int h = lane >> 5, j = lane & 31;
 #pragma unroll
@@ -624,10 +652,11 @@ struct Rows<__bf16, kPlain, D> {
         for (int i = 0; i < 4; ++i) x[i] = o[jt][4 * r4 + i];
         ((floatx4*)region)[(8 * jt + 2 * r4 + h) * kRowTile + j] = x;
       }
-    const float sum = sum_halves(l);
+    const float sum = sum_halves(l), all = kExact ? sum_halves(exact) : 0.f;
     if (h == 0) {
       region[kRowTile * D + j] = m;
       region[kRowTile * D + kRowTile + j] = sum;
+      if (kExact) region[kRowTile * D + 2 * kRowTile + j] = all;
     }
   }
 };
@@ -660,7 +689,7 @@ struct Rows<float, kPlain, D> {
       l[nh] = 0.f;
     }
   }
-  template <bool kInPlace, bool kOnePart>
+  template <bool kInPlace, bool kOnePart, bool kExact>
   __device__ void tile(const uintx4* kt, const uintx4* vt, int n_valid, float c, int lane) {
     const int quarter = lane >> 4, i = lane & 15;
     floatx4 s[2] = {(floatx4)(0.f), (floatx4)(0.f)};
@@ -733,7 +762,9 @@ struct Rows<float, kPlain, D> {
       }
     }
   }
+  template <bool kExact>
   __device__ void put(float* region, int lane) {
+    static_assert(!kExact, "weights are held in binary32");
     const int quarter = lane >> 4, j = lane & 15;
     floatx4* dst = (floatx4*)region;
 #pragma unroll
@@ -767,8 +798,9 @@ struct Rows<float, kPlain, D> {
 // its operands: of K, 32 head dims of one key (the queries are laid out in the same order of the contraction); of V, four head
 // dims of eight keys, a vector of keys for each of the four output tiles (tile jt holds head dims 4 m + jt).  With one or two row
 // tiles nothing is shared between wavefronts: nothing goes through LDS, and a wavefront keeps two tiles of its own in flight.
-// A probability is rounded to bf16 for the output product, as on the interleaved bf16 path (off by 2^-9 of itself at most, a
-// quarter of what the result's own rounding may cost; a second part would take 40 of a tile's vector instructions).
+// A probability is rounded to bf16 for the output product (rounds_weights; a second part would take 40 of a tile's vector
+// instructions).
+template <bool kExact>
 struct Fp4Stream {
   static constexpr int D = 128;
   struct Ids {  // block and slot / 8 in it of the group of eight keys that a lane's K, V and V vectors belong to
@@ -782,7 +814,8 @@ struct Fp4Stream {
   };
   bf16x8 q[D / 16];
   floatx16 o[D / 32];
-  float m, l;  // of row lane % 32; l: this half-wavefront's keys
+  float m, l;   // of row lane % 32; l: this half-wavefront's keys
+  float exact;  // l of unrounded weights
 
   __device__ void begin(const TiledArgs& a, int base, int g, int row0, int rows, int lane) {
     const int h = lane >> 5, j = lane & 31;
@@ -796,7 +829,7 @@ struct Fp4Stream {
 #pragma unroll
     for (int jt = 0; jt < D / 32; ++jt) o[jt] = (floatx16)(0.f);
     m = -INFINITY;
-    l = 0.f;
+    l = exact = 0.f;
   }
   // Row i of the score tile holds key (i & 16) + sigma(i & 15) of the tile: a lane's eight registers are eight consecutive keys.
   // Groups of eight keys lie in one page, so what a vector holds behind the prefix's end is in the page too (and masked);
@@ -831,7 +864,7 @@ struct Fp4Stream {
       r.vs[kk] = *(const uint64_t*)(vp + (uint32_t)(id.vs[kk] * 8 + bs * (D / 2) + (d >> 5) * bs));
     }
   }
-  // The reference, the sum and O follow the 32 scores; the probabilities of a lane's two times eight keys.
+  // The reference, the sums and O follow the 32 scores; the probabilities of a lane's two times eight keys.
   __device__ void softmax(bf16x8 (&pb)[2], const floatx16& s, float c) {
     float mx = s[0];
 #pragma unroll
@@ -841,6 +874,7 @@ struct Fp4Stream {
     if (__any((m_new - m) * c > kRescaleStep)) {
       const float alpha = weight(m, m_new, c);
       l *= alpha;
+      if (kExact) exact *= alpha;
 #pragma unroll
       for (int jt = 0; jt < D / 32; ++jt) o[jt] *= alpha;
       m = m_new;
@@ -851,8 +885,9 @@ struct Fp4Stream {
       floatx8 p;
 #pragma unroll
       for (int e = 0; e < 8; ++e) p[e] = __builtin_amdgcn_exp2f(fmaf(s[8 * kk + e], c, -mc));
-      l += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
+      if (kExact) exact += sum8(p);
       pb[kk] = __builtin_convertvector(p, bf16x8);
+      l = add_bf16(pb[kk], l);
     }
   }
   template <bool kMask>
@@ -1100,15 +1135,16 @@ struct Fp4Stream {
       for (int jt = 0; jt < 4; ++jt) x[jt] = o[jt][i];
       ((floatx4*)region)[(8 * (i >> 2) + 4 * h + (i & 3)) * kRowTile + j] = x;
     }
-    const float sum = sum_halves(l);
+    const float sum = sum_halves(l), all = kExact ? sum_halves(exact) : 0.f;
     if (h == 0) {
       region[kRowTile * D + j] = m;
       region[kRowTile * D + kRowTile + j] = sum;
+      if (kExact) region[kRowTile * D + 2 * kRowTile + j] = all;
     }
   }
 };
 
-constexpr int region_floats(int D) { return kRowTile * (D + 2); }
+constexpr int region_floats(int D, bool exact) { return kRowTile * (D + (exact ? 3 : 2)); }
 
 // ---- finishing a row: the tree part, then the prefix partials ------------------------------------------------------
 // Four elements as they lie in memory (converted where they are used: half the registers for bf16).
@@ -1133,7 +1169,7 @@ __device__ inline int owner_of(const TiledArgs& a, int node) {
 // what does not depend on each other is requested together: the mask and the query while the plan is looked up, the
 // next two tree keys while the last two are used, two partials at a time.  All lanes of a wavefront go through this
 // together (rows that are not `active` have no keys and are not written).
-template <typename T, int D>
+template <typename T, int D, bool kExact>
 struct Finish {
   static constexpr int K4 = D / 32;
   typedef typename Four<T>::type Raw;
@@ -1141,6 +1177,7 @@ struct Finish {
   Raw q[K4];
   floatx4 acc[K4];
   float m = -INFINITY, l = 0.f;
+  float exact = 0.f;  // l of unrounded weights (kExact)
 
   __device__ void clear() {
 #pragma unroll
@@ -1201,21 +1238,23 @@ struct Finish {
       const float al = weight(m, m_new, a.c);
       const float p0 = cur.have[0] ? weight(dot[0], m_new, a.c) : 0.f, p1 = cur.have[1] ? weight(dot[1], m_new, a.c) : 0.f;
       l = l * al + (p0 + p1);
+      if (kExact) exact = exact * al + (p0 + p1);
       m = m_new;
 #pragma unroll
       for (int k = 0; k < K4; ++k) acc[k] = acc[k] * al + (p0 * widen(cur.v[0][k]) + p1 * widen(cur.v[1][k]));
       cur = nxt;
     }
   }
-  // One partial: its max, sum and the row's O, which lies in groups of four elements `stride` floats apart.
+  // One partial: its max, sums and the row's O, which lies in groups of four elements `stride` floats apart.
   struct Partial {
-    float m, l;
+    float m, l, exact;
     floatx4 o[K4];
   };
-  __device__ static Partial fetch(float mc, float lc, const float* o, int stride, int e) {
+  __device__ static Partial fetch(float mc, float lc, float exact, const float* o, int stride, int e) {
     Partial p;
     p.m = mc;
     p.l = lc;
+    p.exact = exact;
 #pragma unroll
     for (int k = 0; k < K4; ++k) p.o[k] = *(const floatx4*)(o + (e + 8 * k) * stride);
     return p;
@@ -1224,6 +1263,7 @@ struct Finish {
     const float m_new = fmaxf(m, p.m);
     const float al = weight(m, m_new, c), wt = weight(p.m, m_new, c);
     l = l * al + p.l * wt;
+    if (kExact) exact = exact * al + p.exact * wt;
 #pragma unroll
     for (int k = 0; k < K4; ++k) acc[k] = acc[k] * al + wt * p.o[k];
     m = m_new;
@@ -1233,7 +1273,7 @@ struct Finish {
     const float inv = l > 0.f ? 1.f / l : 0.f;
 #pragma unroll
     for (int k = 0; k < K4; ++k) store4((T*)a.out + row * D + 4 * (e + 8 * k), acc[k] * inv);
-    if (a.lse && e == 0) a.lse[row] = l > 0.f ? m * a.scale + logf(l) : -INFINITY;
+    if (a.lse && e == 0) a.lse[row] = l > 0.f ? m * a.scale + logf(kExact ? exact : l) : -INFINITY;
   }
   // Whether one of the eight lanes of this row holds an infinity or NaN that does not come from NaN scores (those stay NaN
   // whichever way they are summed).  All lanes of the wavefront take part.
@@ -1293,6 +1333,7 @@ struct Finish {
         }
       f.add_key(k4, v4, have, 1.f, 1.f, a.c);
     }
+    f.exact = f.l;
     if (active) f.write(a, node, head, e);
   }
   // Four elements of the cache: together (and aligned as such, like all chunks of this path), or eight elements apart.
@@ -1353,15 +1394,17 @@ __device__ inline void zero_row(const TiledArgs& a, int64_t row, int e) {
 }
 
 // ---- the prefix kernel ----------------------------------------------------------------------------------------------------
-template <typename T, CacheType kCache, bool kPlain, int D, bool kDirect>
+template <typename T, CacheType kCache, bool kPlain, int D, bool kDirect, bool kExact>
 __global__ __launch_bounds__(kThreads, 2) void tva_tiled_kernel(TiledArgs a) {
   typedef Stager<T, kCache, kPlain, D> Stage;
-  constexpr bool kStream = streams<T>(kCache, D);
+  typedef Fp4Stream<kExact> Stream;
+  constexpr bool kStream = streams<T>(kCache, D), kRounded = rounds_weights<T>(kCache);
+  static_assert(kRounded || !kExact, "one kind of sum");
   constexpr int kStepKeys = step_keys<T>();
-  constexpr int kRegion = region_floats(D);
-  constexpr int kStageBytes = kStream ? 2 * kTilesPerStep * Fp4Stream::kTileVectors * 16 : 2 * 2 * Stage::kStepChunks * 16, kFoldBytes = kWaves * kRegion * 4;
+  constexpr int kRegion = region_floats(D, kExact);
+  constexpr int kStageBytes = kStream ? 2 * kTilesPerStep * Stream::kTileVectors * 16 : 2 * 2 * Stage::kStepChunks * 16, kFoldBytes = kWaves * kRegion * 4;
   __shared__ uintx4 lds[(kStageBytes > kFoldBytes ? kStageBytes : kFoldBytes) / 16];
-  __shared__ float s_ml[2][kGroupRows];
+  __shared__ float s_ml[kExact ? 3 : 2][kGroupRows];
   __shared__ Sums s_part[kWaves];
   const int tid = threadIdx.x, lane = tid & (kWave - 1);
   const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -1502,14 +1545,14 @@ __global__ __launch_bounds__(kThreads, 2) void tva_tiled_kernel(TiledArgs a) {
       const int32_t* table = a.block_table + (int64_t)b * a.max_blocks;
       float* regions = (float*)lds;
       if constexpr (kStream) {
-        Fp4Stream st;
+        Stream st;
         const int my_row0 = row0 + (busy ? rt * kRowTile : 0);
         st.begin(a, sh.base, g, my_row0, rows, lane);
         const bool ends = t1 == sh.steps;  // the piece that ends the segment has the tree part too
         auto tree = [&]() {
           for (int tt = first; ends && tt * 32 < sh.n; tt += shared) st.tree_tile(a, g, sh.base, sh.n, my_row0, rows, tt, lane);
         };
-        if (r >= 3 && t1 - t0 >= Fp4Stream::kShareSteps)
+        if (r >= 3 && t1 - t0 >= Stream::kShareSteps)
           st.run_shared(a, table, g, t0, t1, len, first, busy, lds, wv, lane, tree);
         else if (busy)
           st.run(a, table, g, t0 * kTilesPerStep + first, min(t1 * kTilesPerStep, (len + 31) / 32), shared, len, lane, tree);
@@ -1537,30 +1580,34 @@ __global__ __launch_bounds__(kThreads, 2) void tva_tiled_kernel(TiledArgs a) {
             for (int x = first; x < kTilesPerStep; x += shared) {
               const int n_valid = len - t * kStepKeys - x * Stage::kKeys;
               if (n_valid <= 0) break;
-              rowset.template tile<kCache == kSameType, kCache == kE2M1>(stage + x * Stage::kTileChunks, stage + Stage::kStepChunks + x * Stage::kTileChunks, n_valid,
+              rowset.template tile<kCache == kSameType, kRounded, kExact>(stage + x * Stage::kTileChunks, stage + Stage::kStepChunks + x * Stage::kTileChunks, n_valid,
                                           a.c_stored, lane);
             }
         }
         // fold: the states that share a row tile, in wavefront order
         __syncthreads();
-        rowset.put(regions + wv * kRegion, lane);
+        rowset.template put<kExact>(regions + wv * kRegion, lane);
       }
       __syncthreads();
-      float* slot = kDirect ? nullptr : a.ws + (wg + at.segs_before + (int64_t)g * sh.groups + group) * slot_floats(D);
+      float* slot = kDirect ? nullptr : a.ws + (wg + at.segs_before + (int64_t)g * sh.groups + group) * slot_floats(D, kExact);
       if (tid < r * kRowTile) {
         const float* ml = regions + (tid >> 5) * kRegion + kRowTile * D + (tid & 31);
-        float m = ml[0], l = ml[kRowTile];
+        float m = ml[0], l = ml[kRowTile], exact = kExact ? ml[2 * kRowTile] : 0.f;
         for (int k = 1; k < shared; ++k) {
-          const float mk = ml[k * apart * kRegion], lk = ml[k * apart * kRegion + kRowTile];
-          const float m_new = fmaxf(m, mk);
-          l = l * weight(m, m_new, a.c_stored) + lk * weight(mk, m_new, a.c_stored);
+          const float* mlk = ml + k * apart * kRegion;
+          const float mk = mlk[0], lk = mlk[kRowTile];
+          const float m_new = fmaxf(m, mk), was = weight(m, m_new, a.c_stored), wk = weight(mk, m_new, a.c_stored);
+          l = l * was + lk * wk;
+          if (kExact) exact = exact * was + mlk[2 * kRowTile] * wk;
           m = m_new;
         }
         s_ml[0][tid] = m;
         s_ml[1][tid] = l;
+        if (kExact) s_ml[kExact ? 2 : 1][tid] = exact;
         if (slot) {
           slot[kGroupRows * D + tid] = m * a.m_scale;  // (-inf stays -inf)
           slot[kGroupRows * D + kGroupRows + tid] = l;
+          if (kExact) slot[kGroupRows * D + 2 * kGroupRows + tid] = exact;
         }
       }
       __syncthreads();
@@ -1584,11 +1631,11 @@ __global__ __launch_bounds__(kThreads, 2) void tva_tiled_kernel(TiledArgs a) {
           const bool active = i < group_rows;
           const int rho = row0 + (active ? i : 0);
           const int node = sh.base + rho / a.G, head = g * a.G + rho % a.G;
-          Finish<T, D> f;
+          Finish<T, D, kExact> f;
           f.request(a, node, head, active, e);
           f.tree(a, g, sh.base, kStream ? 0 : sh.n, e);
           if (active && (kStream || t0 < t1))
-            f.merge(f.fetch(s_ml[0][i] * a.m_scale, s_ml[1][i], regions + (i >> 5) * kRegion + (i & 31) * 4, kRowTile * 4, e),
+            f.merge(f.fetch(s_ml[0][i] * a.m_scale, s_ml[1][i], s_ml[kExact ? 2 : 1][i], regions + (i >> 5) * kRegion + (i & 31) * 4, kRowTile * 4, e),
                     a.c);
           if (active) f.write(a, node, head, e);
           const bool again = f.row_overflowed(lane) && active;
@@ -1612,7 +1659,7 @@ __global__ __launch_bounds__(kThreads, 2) void tva_tiled_kernel(TiledArgs a) {
       const int e = tid & (kCombineLanes - 1);
       for (int h0 = 0; h0 < a.Hq; h0 += kThreads / kCombineLanes) {
         const int h = h0 + tid / kCombineLanes;
-        if (owned) Finish<T, D>::walk(a, node * a.Hq + min(h, a.Hq - 1), h < a.Hq, e);
+        if (owned) Finish<T, D, kExact>::walk(a, node * a.Hq + min(h, a.Hq - 1), h < a.Hq, e);
         else if (h < a.Hq) zero_row<T, D>(a, node * a.Hq + h, e);
       }
     }
@@ -1625,12 +1672,12 @@ __global__ __launch_bounds__(kThreads, 2) void tva_tiled_kernel(TiledArgs a) {
 // partials, merged by the first in a fixed order; for launches that leave wavefront slots idle (see finish_parts).
 // kParts = 0: a wavefront per eight rows goes through both.
 constexpr int finish_waves(int parts) { return parts > 0 ? 1 + parts : 4; }
-template <typename T, int D, int kParts>
+template <typename T, int D, int kParts, bool kExact>
 __global__ __launch_bounds__(finish_waves(kParts) * kWave, kParts == 0 ? 2 : 1) void tva_tiled_finish_kernel(TiledArgs a) {
   constexpr int kRows = kWave / kCombineLanes, K4 = D / 32;
   constexpr int kStates = kParts > 0 ? kParts : 1;
   __shared__ floatx4 s_acc[kStates][K4][kWave];
-  __shared__ float s_m[kStates][kRows], s_l[kStates][kRows];
+  __shared__ float s_m[kStates][kRows], s_l[kStates][kRows], s_exact[kExact ? kStates : 1][kRows];
   const int lane = threadIdx.x & (kWave - 1), e = lane & (kCombineLanes - 1);
   const int wv = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
   const int part = kParts > 0 ? wv - 1 : -1;  // -1: the tree part
@@ -1645,7 +1692,7 @@ __global__ __launch_bounds__(finish_waves(kParts) * kWave, kParts == 0 ? 2 : 1) 
   const bool there = row_raw < n_rows;
   const int64_t row = there ? row_raw : n_rows - 1;
   const int node = (int)(row / a.Hq), head = (int)(row % a.Hq), g = head / a.G;
-  Finish<T, D> f;
+  Finish<T, D, kExact> f;
   if (part < 0) f.request(a, node, head, there, e);
   else f.clear();
   const int64_t U = a.plan[0], W = a.plan[1];
@@ -1675,8 +1722,9 @@ __global__ __launch_bounds__(finish_waves(kParts) * kWave, kParts == 0 ? 2 : 1) 
     const int cost = group < sh.groups - 1 ? StepCost<T>::four : sh.cost_last;
     const int64_t w_first = ((ub + cost) * W - 1) / U, w_last = ((ub + (int64_t)sh.steps * cost) * W - 1) / U;
     auto partial = [&](int64_t w) {
-      const float* slot = a.ws + (w + segs_before + local) * slot_floats(D);
-      return f.fetch(slot[kGroupRows * D + r], slot[kGroupRows * D + kGroupRows + r], slot + r * 4, kGroupRows * 4, e);
+      const float* slot = a.ws + (w + segs_before + local) * slot_floats(D, kExact);
+      return f.fetch(slot[kGroupRows * D + r], slot[kGroupRows * D + kGroupRows + r], kExact ? slot[kGroupRows * D + 2 * kGroupRows + r] : 0.f,
+                     slot + r * 4, kGroupRows * 4, e);
     };
     for (int64_t w = w_first + (kParts > 0 ? part : 0); w <= w_last; w += 2 * kStates) {
       const auto p0 = partial(w);
@@ -1693,15 +1741,17 @@ __global__ __launch_bounds__(finish_waves(kParts) * kWave, kParts == 0 ? 2 : 1) 
       if (e == 0) {
         s_m[part][lane / kCombineLanes] = f.m;
         s_l[part][lane / kCombineLanes] = f.l;
+        if (kExact) s_exact[part][lane / kCombineLanes] = f.exact;
       }
     }
     __syncthreads();
     if (part >= 0) return;
 #pragma unroll
     for (int p = 0; p < kParts; ++p) {
-      typename Finish<T, D>::Partial x;
+      typename Finish<T, D, kExact>::Partial x;
       x.m = s_m[p][lane / kCombineLanes];
       x.l = s_l[p][lane / kCombineLanes];
+      x.exact = kExact ? s_exact[kExact ? p : 0][lane / kCombineLanes] : 0.f;
 #pragma unroll
       for (int k = 0; k < K4; ++k) x.o[k] = s_acc[p][k][lane];
       f.merge(x, a.c);
@@ -1728,8 +1778,8 @@ static int64_t tiled_segments(int32_t batch, int32_t total_nodes, int32_t num_q_
   return (int64_t)num_kv_heads * (((int64_t)total_nodes * G + kGroupRows - 1) / kGroupRows + batch);
 }
 
-static size_t partials_bytes(const smart_ctx* ctx, int64_t segs, int32_t head_dim) {
-  return ((size_t)(tiled_workgroups(ctx) + segs + 1) * slot_floats(head_dim) * sizeof(float) + 255) & ~(size_t)255;
+static size_t partials_bytes(const smart_ctx* ctx, int64_t segs, int32_t head_dim, bool exact) {
+  return ((size_t)(tiled_workgroups(ctx) + segs + 1) * slot_floats(head_dim, exact) * sizeof(float) + 255) & ~(size_t)255;
 }
 static size_t plan_bytes(int32_t batch) { return sizeof(int64_t) * (2 + 2 * (size_t)batch); }
 
@@ -1737,7 +1787,7 @@ static size_t plan_bytes(int32_t batch) { return sizeof(int64_t) * (2 + 2 * (siz
 size_t tva_tiled_reserve(const smart_ctx* ctx, int32_t batch, int32_t total_nodes, int32_t num_q_heads,
                          int32_t num_kv_heads) {
   const int64_t segs = ((int64_t)total_nodes * num_q_heads + kGroupRows - 1) / kGroupRows + (int64_t)num_kv_heads * (batch + 1);
-  return partials_bytes(ctx, segs, 128) + plan_bytes(batch);
+  return partials_bytes(ctx, segs, 128, true) + plan_bytes(batch);
 }
 
 // Every 16-byte chunk of a staged row, every query row and every tree row must be addressable with one load.
@@ -1773,21 +1823,21 @@ static int32_t segment_cost(const tva_params& p, int32_t workgroups) {
 // (720 53.5 / 51.0, 756 27.0 / 28.3, 832 44.0 / 42.5); 1500, 16 sequences of 60 .. 128 nodes, 31.9 / 34.6 / 42.7; 2016 42.2 /
 // 47.7 / 70.6; the bf16 workload above (2176) 95.2 / 97.1 / 117.6.
 static int finish_parts(int64_t rows8) { return rows8 <= 128 ? 7 : (rows8 <= 640 ? 1 : 0); }
-template <typename T, int D>
+template <typename T, int D, bool kExact>
 static void launch_finish(const TiledArgs& a, int64_t rows8, hipStream_t stream) {
   const int parts = finish_parts(rows8), waves = finish_waves(parts);
   const dim3 grid((unsigned)(parts > 0 ? rows8 : (rows8 + waves - 1) / waves)), block(waves * kWave);
-  if (parts == 7) hipLaunchKernelGGL((tva_tiled_finish_kernel<T, D, 7>), grid, block, 0, stream, a);
-  else if (parts == 1) hipLaunchKernelGGL((tva_tiled_finish_kernel<T, D, 1>), grid, block, 0, stream, a);
-  else hipLaunchKernelGGL((tva_tiled_finish_kernel<T, D, 0>), grid, block, 0, stream, a);
+  if (parts == 7) hipLaunchKernelGGL((tva_tiled_finish_kernel<T, D, 7, kExact>), grid, block, 0, stream, a);
+  else if (parts == 1) hipLaunchKernelGGL((tva_tiled_finish_kernel<T, D, 1, kExact>), grid, block, 0, stream, a);
+  else hipLaunchKernelGGL((tva_tiled_finish_kernel<T, D, 0, kExact>), grid, block, 0, stream, a);
 }
 
-template <typename T, CacheType kCache, bool kPlain, int D>
+template <typename T, CacheType kCache, bool kPlain, int D, bool kExact = false>
 static hipError_t launch_tiled(const TiledArgs& a, bool direct, unsigned grid, hipStream_t stream) {
   if (direct)
-    hipLaunchKernelGGL((tva_tiled_kernel<T, kCache, kPlain, D, true>), dim3(grid), dim3(kThreads), 0, stream, a);
+    hipLaunchKernelGGL((tva_tiled_kernel<T, kCache, kPlain, D, true, kExact>), dim3(grid), dim3(kThreads), 0, stream, a);
   else
-    hipLaunchKernelGGL((tva_tiled_kernel<T, kCache, kPlain, D, false>), dim3(grid), dim3(kThreads), 0, stream, a);
+    hipLaunchKernelGGL((tva_tiled_kernel<T, kCache, kPlain, D, false, kExact>), dim3(grid), dim3(kThreads), 0, stream, a);
   return hipGetLastError();
 }
 
@@ -1843,7 +1893,8 @@ int32_t tva_launch_tiled(smart_ctx* ctx, hipStream_t stream, const tva_params& p
     direct = capture != hipStreamCaptureStatusNone;
   }
   void* ws = nullptr;
-  const size_t partials = partials_bytes(ctx, segs, p.head_dim);  // then the plan
+  const bool exact = fp4 && !f32 && p.d_lse != nullptr;  // two kinds of sums (rounds_weights)
+  const size_t partials = partials_bytes(ctx, segs, p.head_dim, exact);  // then the plan
   if (!direct) {
     const int32_t rc = tiled_workspace(ctx, stream, partials + plan_bytes(p.batch), &ws);
     if (rc == SMART_EHIP) return rc;
@@ -1907,7 +1958,10 @@ int32_t tva_launch_tiled(smart_ctx* ctx, hipStream_t stream, const tva_params& p
     else if (fp8) { if (plain) SMART_TILED(float, kE4M3, true); else SMART_TILED(float, kE4M3, false); }
     else { if (plain) SMART_TILED(float, kSameType, true); else SMART_TILED(float, kSameType, false); }
   } else {
-    if (fp4) SMART_TILED(__bf16, kE2M1, false);
+    if (exact)
+      err = p.head_dim == 128 ? launch_tiled<__bf16, kE2M1, false, 128, true>(a, direct, grid, stream)
+                              : launch_tiled<__bf16, kE2M1, false, 64, true>(a, direct, grid, stream);
+    else if (fp4) SMART_TILED(__bf16, kE2M1, false);
     else if (fp8) { if (plain) SMART_TILED(__bf16, kE4M3, true); else SMART_TILED(__bf16, kE4M3, false); }
     else { if (plain) SMART_TILED(__bf16, kSameType, true); else SMART_TILED(__bf16, kSameType, false); }
   }
@@ -1916,11 +1970,14 @@ int32_t tva_launch_tiled(smart_ctx* ctx, hipStream_t stream, const tva_params& p
   rc = profile_end(ctx, stream);
   if (rc != SMART_OK || direct) return rc;
   if (f32) {
-    if (p.head_dim == 128) launch_finish<float, 128>(a, rows8, stream);
-    else launch_finish<float, 64>(a, rows8, stream);
+    if (p.head_dim == 128) launch_finish<float, 128, false>(a, rows8, stream);
+    else launch_finish<float, 64, false>(a, rows8, stream);
+  } else if (exact) {
+    if (p.head_dim == 128) launch_finish<__bf16, 128, true>(a, rows8, stream);
+    else launch_finish<__bf16, 64, true>(a, rows8, stream);
   } else {
-    if (p.head_dim == 128) launch_finish<__bf16, 128>(a, rows8, stream);
-    else launch_finish<__bf16, 64>(a, rows8, stream);
+    if (p.head_dim == 128) launch_finish<__bf16, 128, false>(a, rows8, stream);
+    else launch_finish<__bf16, 64, false>(a, rows8, stream);
   }
   SMART_HIP_CHECK(hipGetLastError());
   return SMART_OK;
