@@ -1866,7 +1866,9 @@ int32_t tva_launch_tiled(smart_ctx* ctx, hipStream_t stream, const tva_params& p
   const int64_t step = f32 ? step_keys<float>() : step_keys<__bf16>(), rows = (int64_t)p.total_nodes * G;
   // `segs` is what any offsets can make; trees much alike make `likely` (where the grid is larger, the surplus comes last: then
   // consecutive segments go to different L2s, or those of one L2 would have them all.  30 sequences, 8 kv heads, 8 nodes, 64 tokens 18.0
-  // -> 9.9 us.)
+  // -> 9.9 us.  So also with the other caches, static calls, without / with: plain bf16, the same 24.2 / 13.9, 500 tokens 37.1 / 22.1;
+  // 8 sequences of 100 nodes, whose row groups no longer share an L2, 2000 tokens 157 / 94, fp8 156 / 89, fp32 594 / 303; two of 128
+  // nodes before 28 of two 220 / 121, behind them 218 / 174; fp32, 60 sequences of 4 kv heads 27.0 / 27.0.)
   // With a 4-bit cache and bf16.  Where the operands stream from the pages a workgroup takes as long as its keys times its row tiles (1, 2, or 4 for three and
   // four), 4.4 ns each, and the split form 9 us more than its share of all keys; of lengths that differ as 1 .. 2 do the longest is
   // spent on all: direct up to 2048 / (1 - 0.8 likely / compute units) keys of one row tile.  32 / 8 heads of 128, equal lengths, split and
