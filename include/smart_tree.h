@@ -836,7 +836,9 @@ int32_t tree_commit_fp4(smart_ctx* ctx, void* stream, int32_t src_dtype,
  * workspace: it may be captured, and calls may run at the same time.
  * Host errors: SMART_EINVAL for null pointers, Hq % Hkv != 0, head_dim not in
  * {64, 128}, unknown dtype, softmax_scale not positive or not below 1e30,
- * total_tokens x Hq >= 2^31, token strides smaller than a token's row, k_stride or
+ * total_tokens x Hq >= 2^31, more prompts than a grid holds (num_kv_heads x batch
+ * from 2^23 on with fp32 or large calls of head_dim 128, else from 2^24), token
+ * strides smaller than a token's row, k_stride or
  * v_stride of 2^24 elements or more, pointers or token strides that are not multiples
  * of 16 bytes; SMART_EHIP.
  * ------------------------------------------------------------------------- */

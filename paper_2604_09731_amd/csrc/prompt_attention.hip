@@ -729,9 +729,7 @@ int64_t most_tiles(const PromptArgs& a, int rows) { return (int64_t)a.total_toke
 
 template <typename Kernel>
 int32_t launch(Kernel kernel, int threads, int rows, const PromptArgs& a, hipStream_t stream) {
-  const int64_t grid = most_tiles(a, rows) * a.Hkv;
-  if (grid > 0x7FFFFFFF) return SMART_EINVAL;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(threads), 0, stream, a);
+  hipLaunchKernelGGL(kernel, dim3((unsigned)(most_tiles(a, rows) * a.Hkv)), dim3(threads), 0, stream, a);
   SMART_HIP_CHECK(hipGetLastError());
   return SMART_OK;
 }
@@ -749,11 +747,16 @@ int32_t launch_rows(const PromptArgs& a, hipStream_t stream) {
 // 3690; head dim 64, 8 heads, one of 4096 34.6 / 46.1 / 74.0, 64 of 1 .. 300 14.7 / 11.7 / 14.9, 4 of 1024 .. 2048 26.4 / 34.3 / 52.4;
 // 32 heads, 4 of 4096 383 / 309 / 289.  (Two teams of wavefronts on one row tile, with half of the keys each, are ahead for a few
 // prompts of few heads only: one of 4096, 8 heads of 64, 27 for 35 us; one of 2048, 32 heads of 128, 51; 8262 tokens 212.)
-template <int D>
-int32_t launch_bf16(const PromptArgs& a, hipStream_t stream) {
+int tile_rows(const PromptArgs& a, bool f32) {
   const int64_t rows = (int64_t)a.total_tokens * a.Hq, cus = a.num_cus;
-  if (rows <= 192 * cus) return launch_rows<D, 4, 1>(a, stream);
-  if (rows < 4 * 256 * cus) return launch_rows<D, 4, 2>(a, stream);
+  return f32 || rows <= 192 * cus ? 64 : (rows < 4 * 256 * cus ? 128 : 256);
+}
+int tile_threads(int rows, bool f32, int D) { return f32 || (rows == 256 && D == 128) ? 512 : 256; }
+
+template <int D>
+int32_t launch_bf16(const PromptArgs& a, int rows, hipStream_t stream) {
+  if (rows == 64) return launch_rows<D, 4, 1>(a, stream);
+  if (rows == 128) return launch_rows<D, 4, 2>(a, stream);
   return launch_rows<D, D == 128 ? 8 : 4, D == 128 ? 2 : 4>(a, stream);
 }
 
@@ -801,14 +804,17 @@ extern "C" int32_t prompt_attention(smart_ctx* ctx, void* stream, const prompt_p
   a.num_cus = ctx->num_cus > 0 ? ctx->num_cus : 256;
   a.scale = p.softmax_scale;
   a.c = p.softmax_scale * kLog2e;
+  const bool f32 = p.dtype == SMART_F32;
+  const int rows = tile_rows(a, f32), threads = tile_threads(rows, f32, p.head_dim);
+  if (most_tiles(a, rows) * a.Hkv > 0xFFFFFFFFll / threads) return SMART_EINVAL;  // (a grid's threads are counted in 32 bits)
   int prev = 0;
   SMART_HIP_CHECK(hipGetDevice(&prev));
   if (prev != ctx->device) SMART_HIP_CHECK(hipSetDevice(ctx->device));
   hipStream_t s = (hipStream_t)stream;
-  if (p.dtype == SMART_F32) {
-    rc = p.head_dim == 128 ? launch(prompt_f32_kernel<128>, 512, 64, a, s) : launch(prompt_f32_kernel<64>, 512, 64, a, s);
+  if (f32) {
+    rc = p.head_dim == 128 ? launch(prompt_f32_kernel<128>, threads, rows, a, s) : launch(prompt_f32_kernel<64>, threads, rows, a, s);
   } else {
-    rc = p.head_dim == 128 ? launch_bf16<128>(a, s) : launch_bf16<64>(a, s);
+    rc = p.head_dim == 128 ? launch_bf16<128>(a, rows, s) : launch_bf16<64>(a, rows, s);
   }
   if (prev != ctx->device) (void)hipSetDevice(prev);
   return rc;
