@@ -564,7 +564,7 @@ int32_t kv_cache_write_fp8(smart_ctx* ctx, void* stream, int32_t src_dtype, int3
  * codes and scales.
  * Errors: SMART_EINVAL (null pointers, sizes, dtype; caches, strides, sources
  * and destinations that are not aligned to 16 bytes; strides smaller than a
- * page).
+ * page; 2^27 tokens and more; rows of 2^24 elements and more).
  * ------------------------------------------------------------------------- */
 int32_t kv_cache_write_fp4(smart_ctx* ctx, void* stream, int32_t src_dtype, int32_t n_tokens,
                            int32_t num_kv_heads, int32_t head_dim, int32_t block_size, int32_t num_blocks,

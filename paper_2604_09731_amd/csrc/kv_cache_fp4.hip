@@ -201,7 +201,7 @@ __global__ __launch_bounds__(kThreads) void tree_commit_fp4_kernel(Pages pg, sma
 bool copy_grid(int32_t n_tokens, int32_t num_kv_heads, int32_t head_dim, dim3* grid) {
   const int64_t x = ((int64_t)n_tokens + kTokens - 1) / kTokens, piece = kWaves * kDims;
   const int64_t y = ((int64_t)num_kv_heads * head_dim + piece - 1) / piece;
-  if (y > 65535) return false;
+  if (y > 65535 || x * kThreads > 0xFFFFFFFFll) return false;  // (a grid's threads are counted in 32 bits)
   *grid = dim3((unsigned)x, (unsigned)y);
   return true;
 }
