@@ -557,7 +557,8 @@ int32_t kv_cache_write_fp8(smart_ctx* ctx, void* stream, int32_t src_dtype, int3
  * to x / scale, ties to the even code, saturating at +-6 (infinities too); a
  * NaN makes all 32 NaN.  Head dims, kv heads and tokens do not share anything.
  * Reading: row t of d_k_dst / d_v_dst ([n_tokens][num_kv_heads][head_dim], of
- * dst_dtype; every value is exact in both types) is the row of slot
+ * dst_dtype; every value that writing stores is exact in both types, others past
+ * binary32 read as infinite) is the row of slot
  * d_slot_mapping[t]; rows of negative slots and of slots outside the cache
  * become zero.
  * A slot that one writing call names twice holds afterwards any mix of the rows'
@@ -587,7 +588,8 @@ int32_t kv_cache_read_fp4(smart_ctx* ctx, void* stream, int32_t dst_dtype, int32
  *            followed by the tree nodes j of b with bit j set in anc_mask[i]
  *            (i itself and its ancestors)
  *   out[i,h,:] = softmax_keys(softmax_scale * <q[i,h,:], k[g,:]>) . v[g,:]
- *   lse[i,h]   = log sum_keys exp(score)                      (optional)
+ *   lse[i,h]   = log sum_keys exp(score)                      (optional; -infinity for a
+ *                row without keys, and for one with a score of NaN, which is NaN itself)
  * Scores, softmax and accumulation are fp32 (bf16 inputs are multiplied on
  * the matrix cores with fp32 accumulation; the kernel for bf16 / interleaved /
  * block_size 16 / head_dim 128 rounds softmax weights to bf16 before the second

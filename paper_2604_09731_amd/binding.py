@@ -463,7 +463,8 @@ def interleave_kv_cache(k_plain, v_plain):
 
 
 def fp4_page_bytes(block_size: int, head_dim: int) -> int:
-    """Bytes of a page (one block and kv head, of K or of V) of a 4-bit cache: the codes and the scale bytes behind them."""
+    """Bytes of a page (one block and kv head, of K or of V) of a 4-bit cache: the codes and the scale bytes behind them.
+    The caches' strides are multiples of 16, which this is but for a block size of 8 and an odd multiple of 32 head dims."""
     return block_size * head_dim // 2 + block_size * head_dim // 32
 
 
@@ -581,7 +582,8 @@ class SmartTree:
             raise ValueError(f"expected tensors on this handle's GPU, got one on {t.device}")
 
     def kv_cache_write_fp4(self, k_src, v_src, slot_mapping, k_cache, v_cache, block_size):
-        """Rows [n, Hkv, D] into 4-bit caches: uint8 tensors [num_blocks, Hkv, fp4_page_bytes(block_size, D)]."""
+        """Rows [n, Hkv, D] into 4-bit caches: uint8 tensors [num_blocks, Hkv, fp4_page_bytes(block_size, D)] or more, of
+        strides that are multiples of 16."""
         self._here(k_src)
         self._native.cache_write_fp4(self._ctx, k_src, v_src, slot_mapping, k_cache, v_cache, block_size)
 

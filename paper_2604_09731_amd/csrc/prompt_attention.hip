@@ -6,7 +6,7 @@
 // time: one pass with the running maximum and sum of a softmax, keys and values staged through LDS.
 //   * Scores are kept transposed (keys x rows): a row's softmax stays inside the four lanes of a column, and the
 //     probabilities come out in the operand layout of the second product.
-//   * Row tiles are handed out from the longest down: what is dispatched last is short.
+//   * Row tiles are handed out from the longest down, of up to 64 prompts: what is dispatched last is short.
 //   * Bound by the matrix cores: 4 D flops per (row, key).
 //   * Values of later tokens are multiplied by probabilities of zero where a tile crosses the diagonal; a row that comes out
 //     infinite or NaN is evaluated once more over its own keys only (evaluate_again).
@@ -123,7 +123,8 @@ __device__ inline Item find_item(const PromptArgs& a, int rank) {
     it.tile = lo;
     return it;
   }
-  // more prompts: one after the other, each from its last tile down
+  // More prompts: one after the other, each from its last tile down, and all offsets in every workgroup.  64 prompts of 300 tokens, 32
+  // / 8 heads of 128, 160 us, 65 214; 64 of 100 before one of 4000 214, behind it 206; 1000 of 1 .. 8 tokens 19, 20000 2867.
   const int tid = threadIdx.x, each = (a.batch + kThreads - 1) / kThreads;
   if (tid == 0) s_bad = 0, s_item = it;
   __syncthreads();
