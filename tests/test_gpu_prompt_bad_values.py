@@ -31,7 +31,8 @@ def _some_rows(out, q, k, v, lo, tokens, heads, scale, dtype):
             assert np.array_equal(got[np.isinf(ref)], ref[np.isinf(ref)]), (t, h)
             u = (2 * D * S + 2 * (t + 1 - lo) + 16) * U
             tol = u * A + (2 * 2.0 ** -8 * A + 2.0 ** -8 * np.abs(ref) if dtype == "bf16" else U * np.abs(ref))
-            assert (np.abs(got - ref)[good] <= tol[good]).all(), (t, h, np.nanmax(np.abs(got - ref)[good] / tol[good]))
+            off = np.abs(got[good] - ref[good])
+            assert (off <= tol[good]).all(), (t, h, (off / tol[good]).max())
 
 
 @pytest.mark.parametrize("dtype,D,lens", [("bf16", 128, [300, 90]), ("bf16", 64, [1030]), ("f32", 64, [300, 90]), ("f32", 128, [260])])
