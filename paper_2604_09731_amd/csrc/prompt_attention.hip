@@ -13,12 +13,16 @@
 #include <math.h>
 
 #include "common.h"
+#include "wave.h"
 
 namespace {
 
+using smart::add_pair;
+using smart::max_quarters;
+using smart::sum_quarters;
+
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
 typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
-typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 typedef __attribute__((ext_vector_type(4))) short shortx4;
 typedef __attribute__((ext_vector_type(4))) float floatx4;
 typedef __attribute__((ext_vector_type(8))) float floatx8;
@@ -44,23 +48,6 @@ struct PromptArgs {
   uint32_t num_cus;
   float scale, c;  // c: in powers of two
 };
-
-__device__ inline float max_halves(float x) {
-  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
-}
-__device__ inline float sum_halves(float x) {
-  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
-}
-__device__ inline float max_quarters(float x) {  // over the lanes with the same lane % 16
-  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return max_halves(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
-}
-__device__ inline float sum_quarters(float x) {
-  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return sum_halves(__uint_as_float(r[0]) + __uint_as_float(r[1]));
-}
 
 // `op` over the 64 lanes, the same in all of them: lanes 1, 2, 4 and 8 apart by data-parallel moves, 16 and 32 apart by swaps.
 template <typename Op>
@@ -444,10 +431,6 @@ __global__ __launch_bounds__(512, D == 64 ? 4 : 2) void prompt_f32_kernel(Prompt
 }
 
 // ---- bf16 -----------------------------------------------------------------------------------------------------------------
-// Two bf16 ones: the sum of a pair of rounded probabilities is one dot product.
-__device__ inline float add_pair(uint32_t pair, float sum) {
-  return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pair), __builtin_bit_cast(bf16x2, 0x3F803F80u), sum, false);
-}
 __device__ inline float highest(const floatx8& x) {
   return fmaxf(fmaxf(fmaxf(fmaxf(x[0], x[1]), x[2]), fmaxf(x[3], x[4])), fmaxf(fmaxf(x[5], x[6]), x[7]));
 }

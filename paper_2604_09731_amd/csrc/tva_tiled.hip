@@ -53,6 +53,12 @@
 
 namespace {
 
+using smart::add_pair;
+using smart::max_halves;
+using smart::max_quarters;
+using smart::sum_halves;
+using smart::sum_quarters;
+
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
 typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
 typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
@@ -197,27 +203,6 @@ __device__ inline int clamp_block(int b, int num_blocks) { return b < 0 ? 0 : (b
 // keys: swapping bits 2 and 3 makes the eight registers a lane ends up with eight consecutive keys.
 __device__ inline int sigma(int m) { return (m & 3) | ((m & 4) << 1) | ((m & 8) >> 1); }
 
-__device__ inline float max_halves(float x) {
-  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
-}
-__device__ inline float sum_halves(float x) {
-  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
-}
-__device__ inline float max_rows16(float x) {  // over the lanes with the same lane % 16
-  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return max_halves(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
-}
-__device__ inline float sum_rows16(float x) {
-  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return sum_halves(__uint_as_float(r[0]) + __uint_as_float(r[1]));
-}
-
-// `sum` and a pair of bf16.
-__device__ inline float add_pair(uint32_t pair, float sum) {
-  return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pair), __builtin_bit_cast(bf16x2, 0x3F803F80u), sum, false);
-}
 __device__ inline float add_bf16(bf16x8 x, float sum) {
   const uintx4 pairs = __builtin_bit_cast(uintx4, x);
 #pragma unroll
@@ -716,7 +701,7 @@ struct Rows<float, kPlain, D> {
         for (int r = 0; r < 4; ++r)
           if (4 * quarter + r >= n_valid) s[nh][r] = -INFINITY;
       }
-      const float mx = max_rows16(fmaxf(fmaxf(s[nh][0], s[nh][1]), fmaxf(s[nh][2], s[nh][3])));
+      const float mx = max_quarters(fmaxf(fmaxf(s[nh][0], s[nh][1]), fmaxf(s[nh][2], s[nh][3])));
       m_new[nh] = fmaxf(m[nh], mx);
       move = move || (m_new[nh] - m[nh]) * c > kRescaleStep;
     }
@@ -784,7 +769,7 @@ struct Rows<float, kPlain, D> {
 #pragma unroll
         for (int t = 0; t < D / 16; ++t) dst[(4 * t + quarter) * kRowTile + row] = o[nh][t];
       }
-      const float sum = sum_rows16(l[nh]);
+      const float sum = sum_quarters(l[nh]);
       if (quarter == 0) {
         region[kRowTile * D + row] = m[nh];
         region[kRowTile * D + kRowTile + row] = sum;

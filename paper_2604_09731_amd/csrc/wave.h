@@ -1,4 +1,4 @@
-// Wavefront helpers shared by the kernels that plan for themselves.
+// Wavefront helpers shared by the attention kernels.
 #ifndef SMART_WAVE_H_
 #define SMART_WAVE_H_
 
@@ -41,6 +41,30 @@ __device__ inline int64_t wave_excl_scan(int64_t v, int lane, int64_t* total) {
   incl = dpp_add<0x143, 0xc>(incl);  // row_bcast:31 into rows 2 and 3
   *total = readlane64(incl, 63);
   return incl - v;
+}
+
+// Over the two lanes with the same lane % 32, and over the four with the same lane % 16: the result in each of them.
+__device__ inline float max_halves(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ inline float sum_halves(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+__device__ inline float max_quarters(float x) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return max_halves(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
+}
+__device__ inline float sum_quarters(float x) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return sum_halves(__uint_as_float(r[0]) + __uint_as_float(r[1]));
+}
+
+// `sum` and the two bf16 of a pair: one dot product with two ones, rounded to nearest.
+__device__ inline float add_pair(uint32_t pair, float sum) {
+  typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+  return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pair), __builtin_bit_cast(bf16x2, 0x3F803F80u), sum, false);
 }
 
 }  // namespace smart
