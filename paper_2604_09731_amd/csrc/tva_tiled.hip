@@ -989,7 +989,7 @@ struct Fp4Stream {
   // ---- three and four row tiles: the conversions shared through LDS ----
   // A step's four tiles lie as the lanes take them, 16 bytes a lane: of a tile the eight operands of the scores, then the eight of the
   // output product.  Wavefront w converts the keys of tile w % 4 (w < 4) or its values.  160 vector instructions a wavefront and tile
-  // where every wavefront converting for itself takes 260: 32 sequences of 2048 .. 4096 tokens, 32 / 8 heads, 32 nodes 99 -> 91 us, 128
+  // where every wavefront converting for itself takes 260 (both before the sums became dot products, 14 fewer): 32 sequences of 2048 .. 4096 tokens, 32 / 8 heads, 32 nodes 99 -> 91 us, 128
   // nodes 356 -> 320, 4 .. 64 nodes 117.7 -> 109.2.  The barrier of every step and the first conversions cost more than that in a short
   // piece: 4 sequences, 20 nodes, 35.0 us without, 37.5 with all pieces so, 36.3 with those of five steps and more.  Two row tiles: 59.6
   // without, 69.1.  (What is left: a wavefront's own chain of scores, exponentials and output product; two of them on a SIMD leave
