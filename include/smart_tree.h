@@ -31,6 +31,9 @@
  *                          advances the prefix lengths (closes the step's loop)
  *   prompt_attention       causal attention of whole prompts (the prefill whose
  *                          K/V rows become the cached prefix)
+ *   tree_norm_rope         norms each head of queries and keys and rotates it
+ *   kv_cache_extend,       block tables and slot maps from request lengths, and
+ *   kv_cache_release       pages back to the list of free ones
  *
  * Conventions
  *   - Every function returns int32_t: SMART_OK (0) or a negative error code.
@@ -858,6 +861,107 @@ typedef struct {
 } prompt_params;
 
 int32_t prompt_attention(smart_ctx* ctx, void* stream, const prompt_params* params);
+
+/* ---------------------------------------------------------------------------
+ * tree_norm_rope (device)
+ *
+ * The norm of every head of the queries and keys and the rotation of tree_rope
+ * in one pass, for target models that norm before they rotate: head x of a
+ * token becomes
+ *   y = x / sqrt(mean(x^2) + eps) * weight     (weight [head_dim], NULL: ones),
+ * and pair i of y's first rotary_dim elements is turned by
+ * d_position[t] * base^(-2 i / rotary_dim), paired as for tree_rope.  Angles are
+ * formed in binary64, everything else in binary32; a bf16 result is rounded
+ * once.  A token may be a node of a tree or of a prompt; positions may be any.
+ * q_out / k_out may be q / k themselves, with the same token stride; they
+ * overlap nothing else.  Token strides count elements (heads and head dims are
+ * contiguous), so q and k may be parts of one projection's output.  Uses no
+ * workspace.
+ * Host errors: SMART_EINVAL (null pointers, where there are heads; head counts
+ * negative, both zero or together above 65535; head_dim odd or outside 2 .. 128;
+ * rotary_dim odd or outside 2 .. head_dim; unknown dtype / pairing; base not
+ * positive; eps not positive or not below 1e30; token strides smaller than a
+ * token's row; results in place with another stride; pointers that are not
+ * aligned to an element); SMART_EHIP.  Rows that are aligned to 16 bytes are
+ * fastest.
+ * ------------------------------------------------------------------------- */
+typedef struct {
+  int32_t dtype; /* SMART_F32 | SMART_BF16: q, k, weights and results share it */
+  int32_t n_tokens, num_q_heads, num_kv_heads, head_dim, rotary_dim, pairing;
+  float eps;
+  double base;
+  const int32_t* d_position; /* [n_tokens] */
+  const void* d_q;
+  const void* d_k;
+  const void* d_q_weight; /* [head_dim] or NULL */
+  const void* d_k_weight;
+  void* d_q_out;
+  void* d_k_out;
+  int64_t q_stride, k_stride, q_out_stride, k_out_stride; /* elements from one token to the next */
+} norm_rope_params;
+
+int32_t tree_norm_rope(smart_ctx* ctx, void* stream, const norm_rope_params* params);
+
+/* ---------------------------------------------------------------------------
+ * kv_cache_extend, kv_cache_release (device)
+ *
+ * Who holds which page of the paged cache, kept on the device: d_block_table
+ * [batch][max_blocks_per_seq], of whose row b the first held[b] entries have been
+ * handed out, and a list of free pages, the first free_count[0] entries of
+ * d_free_blocks [free_cap].  Both calls go through the sequences in order, and
+ * their results depend on nothing but their inputs.
+ *
+ * kv_cache_extend makes room for new_tokens[b] tokens behind the len[b] that
+ * sequence b has, and says where they go (before kv_cache_write of a prompt, or
+ * before tree_commit: new_tokens = max_depth + 1).  A sequence that needs blocks
+ * beyond those it holds, ceil((len + new) / block_size) - held of them, takes
+ * them from the end of the list, the last one first.
+ *   d_cu_tokens [batch+1]        running sum of new_tokens, at most total_cap
+ *   d_slot_mapping [total_cap]   of token i of sequence b, in row cu_tokens[b] +
+ *                                i: block * block_size + slot of position len[b]
+ *                                + i; -1 for tokens that got no room, for blocks
+ *                                outside [0, num_blocks), and in rows behind the
+ *                                last token (kv_cache_write skips these)
+ *   d_new_len, d_new_held        len + new_tokens, and held + the blocks taken
+ *   d_status[b]                  SMART_OK; SMART_ECAP if the table's row, the
+ *                                rows up to total_cap or the free blocks (those
+ *                                that the sequences before left over; once they
+ *                                do not suffice for one, no later one gets any)
+ *                                do not suffice; SMART_EINVAL for numbers that
+ *                                are negative, held above max_blocks_per_seq, or
+ *                                len above held * block_size.  With SMART_ECAP or
+ *                                SMART_EINVAL a sequence keeps what it has.
+ * Entries of the block table that are not taken, and the list, stay as they are.
+ *
+ * kv_cache_release gives pages back: of a sequence with finished[b] != 0
+ * (d_finished may be NULL) all; of the others, with window > 0, those that hold
+ * neither one of the first `sinks` tokens nor a token that a node at position
+ * len[b] or later sees through the window (tree_verify_attention_window,
+ * prompt_attention_window).  They are put behind the list's last page, in the
+ * table's order.  Their entries of the table stay and are not to be used again;
+ * released[b] counts the table's entries up to the last one that the window has
+ * left, 0 at first.  Every call for a batch has the same window and sinks.
+ *   d_new_len, d_new_held, d_new_released   0 for a finished sequence
+ *   d_status[b]                  SMART_OK; SMART_ECAP if the list has no room for
+ *                                them (then no later one gives any back either);
+ *                                SMART_EINVAL as above or for released outside
+ *                                0 .. held; such a sequence keeps what it has.
+ * In both, free counts are taken within 0 .. free_cap, d_new_free_count[0] is the
+ * new one, and results alias none of the numbers read.  No workspace.
+ * Host errors: SMART_EINVAL (null pointers, negative sizes, block_size < 1,
+ * max_blocks_per_seq * block_size or total_cap above 2^31 - 1, results that alias
+ * the numbers; window or sinks negative, sinks without a window); SMART_EHIP.
+ * ------------------------------------------------------------------------- */
+int32_t kv_cache_extend(smart_ctx* ctx, void* stream, int32_t batch, int32_t block_size, int32_t max_blocks_per_seq,
+                        int32_t num_blocks, const int32_t* d_len, const int32_t* d_new_tokens, const int32_t* d_held,
+                        const int32_t* d_free_blocks, int32_t free_cap, const int32_t* d_free_count, int32_t* d_block_table,
+                        int64_t total_cap, int32_t* d_cu_tokens, int64_t* d_slot_mapping, int32_t* d_new_len,
+                        int32_t* d_new_held, int32_t* d_new_free_count, int32_t* d_status);
+int32_t kv_cache_release(smart_ctx* ctx, void* stream, int32_t batch, int32_t block_size, int32_t max_blocks_per_seq,
+                         int32_t window, int32_t sinks, const int32_t* d_len, const int32_t* d_held, const int32_t* d_released,
+                         const int32_t* d_finished /* may be NULL */, const int32_t* d_block_table, int32_t* d_free_blocks,
+                         int32_t free_cap, const int32_t* d_free_count, int32_t* d_new_len, int32_t* d_new_held,
+                         int32_t* d_new_released, int32_t* d_new_free_count, int32_t* d_status);
 
 #ifdef __cplusplus
 }

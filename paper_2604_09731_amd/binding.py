@@ -35,7 +35,8 @@ EXPORTS = ["smart_strerror", "smart_last_hip_error", "smart_create", "smart_dest
            "smart_select_begin_device", "smart_select_layer_device", "tree_compact_pack", "tree_compact_pack_fill", "tree_rope", "smart_cost_tables", "smart_cost_tables_biased", "smart_fit_cost_models", "tree_upload",
            "tree_upload_pack", "tree_pack",
            "kv_cache_write", "kv_cache_write_fp8", "tree_verify_attention", "tree_verify_attention_static", "tree_accept", "tree_accept_sample", "tree_commit", "tree_commit_fp8",
-           "kv_cache_write_fp4", "kv_cache_read_fp4", "tree_commit_fp4", "prompt_attention"]
+           "kv_cache_write_fp4", "kv_cache_read_fp4", "tree_commit_fp4", "prompt_attention",
+           "tree_norm_rope", "kv_cache_extend", "kv_cache_release"]
 
 
 class SmartError(RuntimeError):
@@ -75,6 +76,19 @@ class PromptParams(ctypes.Structure):
         ("q_stride", ctypes.c_int64), ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64),
         ("out_stride", ctypes.c_int64),
         ("d_cu_tokens", ctypes.c_void_p), ("d_out", ctypes.c_void_p), ("d_lse", ctypes.c_void_p),
+    ]
+
+
+class NormRopeParams(ctypes.Structure):
+    _fields_ = [
+        ("dtype", ctypes.c_int32), ("n_tokens", ctypes.c_int32), ("num_q_heads", ctypes.c_int32),
+        ("num_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("rotary_dim", ctypes.c_int32),
+        ("pairing", ctypes.c_int32), ("eps", ctypes.c_float), ("base", ctypes.c_double),
+        ("d_position", ctypes.c_void_p), ("d_q", ctypes.c_void_p), ("d_k", ctypes.c_void_p),
+        ("d_q_weight", ctypes.c_void_p), ("d_k_weight", ctypes.c_void_p),
+        ("d_q_out", ctypes.c_void_p), ("d_k_out", ctypes.c_void_p),
+        ("q_stride", ctypes.c_int64), ("k_stride", ctypes.c_int64),
+        ("q_out_stride", ctypes.c_int64), ("k_out_stride", ctypes.c_int64),
     ]
 
 
@@ -178,6 +192,12 @@ def _lib():
                                         vp, vp, i64, i64, vp, vp]
         lib.prompt_attention.restype = i32
         lib.prompt_attention.argtypes = [vp, vp, ctypes.POINTER(PromptParams)]
+        lib.tree_norm_rope.restype = i32
+        lib.tree_norm_rope.argtypes = [vp, vp, ctypes.POINTER(NormRopeParams)]
+        lib.kv_cache_extend.restype = i32
+        lib.kv_cache_extend.argtypes = [vp, vp, i32, i32, i32, i32, vp, vp, vp, vp, i32, vp, vp, i64, vp, vp, vp, vp, vp, vp]
+        lib.kv_cache_release.restype = i32
+        lib.kv_cache_release.argtypes = [vp, vp, i32, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, i32, vp, vp, vp, vp, vp, vp]
         lib.tree_accept.restype = i32
         lib.tree_accept.argtypes = [vp, vp, i32, i32, vp, vp, vp, vp, vp, vp, vp]
         _libh = lib
@@ -410,7 +430,8 @@ _ROW = 128      # int32 elements
 _NATIVE_ENTRIES = ("smart_select_begin_device", "smart_select_layer_device", "tree_compact_pack_fill", "tree_upload_pack",
                    "tree_rope", "kv_cache_write", "kv_cache_write_fp8", "tree_verify_attention",
                    "tree_verify_attention_static", "tree_accept", "tree_accept_sample", "tree_commit", "tree_commit_fp8",
-                   "kv_cache_write_fp4", "kv_cache_read_fp4", "tree_commit_fp4", "prompt_attention")
+                   "kv_cache_write_fp4", "kv_cache_read_fp4", "tree_commit_fp4", "prompt_attention",
+                   "tree_norm_rope", "kv_cache_extend", "kv_cache_release")
 _nativeh = None
 
 
@@ -549,6 +570,32 @@ class SmartTree:
     def tree_rope(self, position, q, k_tree, base=10000.0, rotary_dim=None, pairing=SMART_ROPE_HALF_SPLIT):
         """Rotates q [N, Hq, D] and k_tree [N, Hkv, D] in place by the nodes' position ids."""
         self._native.rope(self._ctx, position, q, k_tree, base, rotary_dim, pairing)
+
+    # -- tree_norm_rope ----------------------------------------------------
+    def tree_norm_rope(self, position, q, k, q_weight, k_weight, eps=1e-6, base=10000.0, rotary_dim=None,
+                       pairing=SMART_ROPE_HALF_SPLIT, q_out=None, k_out=None):
+        """Every head of q [N, Hq, D] and k [N, Hkv, D] (tokens may be strided, as parts of one projection's output are)
+        over its root mean square, times q_weight / k_weight [D] (None: ones), rotated by position [N] (int32).  Returns
+        (q, k), contiguous unless q_out / k_out are given, which may be q and k themselves."""
+        self._here(q)
+        return self._native.norm_rope(self._ctx, position, q, k, q_weight, k_weight, eps, base, rotary_dim, pairing, q_out, k_out)
+
+    # -- kv_cache_extend, kv_cache_release ---------------------------------
+    def kv_cache_extend(self, length, new_tokens, held, block_table, free_blocks, free_count, block_size, num_blocks, total_cap):
+        """Room for new_tokens[b] tokens behind length[b] (all int32, on the device): block_table [B, blocks] gets the blocks
+        that the sequences lack, from the end of the first free_count[0] of free_blocks.  Returns (cu_tokens [B + 1],
+        slot_mapping int64 [total_cap], new length, new held, new free_count [1], status [B])."""
+        self._here(length)
+        return self._native.cache_extend(self._ctx, length, new_tokens, held, block_table, free_blocks, free_count, block_size,
+                                         num_blocks, total_cap)
+
+    def kv_cache_release(self, length, held, released, block_table, free_blocks, free_count, block_size, finished=None, window=0,
+                         sinks=0):
+        """Blocks of finished sequences, and those that a window (0: none) has left, behind the first free_count[0] of
+        free_blocks (in place).  Returns (new length, new held, new released, new free_count [1], status [B])."""
+        self._here(length)
+        return self._native.cache_release(self._ctx, length, held, released, block_table, free_blocks, free_count, block_size,
+                                          finished, window, sinks)
 
     # -- tree_pack ---------------------------------------------------------
     def tree_pack(self, cu_nodes, parent, prefix_len):

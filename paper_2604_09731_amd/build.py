@@ -20,7 +20,8 @@ OBJ_DIR = os.path.join(HERE, "_build")
 
 HIP_SOURCES = ["smart_ctx.hip", "tree_pack_accept.hip", "kv_cache_write.hip", "tva_general.hip",
                "tva_mfma.hip", "tva_tiled.hip", "tva_api.hip", "tva_static.hip", "smart_select_device.hip", "tree_rope.hip",
-               "tree_accept_sample.hip", "kv_cache_fp4.hip", "prompt_attention.hip"]
+               "tree_accept_sample.hip", "kv_cache_fp4.hip", "prompt_attention.hip",
+               "tree_norm_rope.hip", "kv_cache_blocks.hip"]
 HOST_SOURCES = ["smart_select.cpp", "smart_cost_model.cpp"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

@@ -1,8 +1,8 @@
 // The binding's calls in native code: output allocation, argument marshalling and the library call of the device entry
 // points, for binding.py.  A small call waits for the host, not for the GPU (a draft layer's kernel takes 4.8 us, the call took
 // 7.5 us of host time, of which the launch is 3.3): each output tensor made and each address passed from Python costs 0.1 ..
-// 1.4 us there.  No arithmetic; the calls on 4-bit caches and prompt_attention check their tensors' shapes, types, strides and
-// devices here, the others nothing beyond what the Python side checked.  The entry points come as addresses, so that this module
+// 1.4 us there.  No arithmetic; the calls on 4-bit caches, prompt_attention, tree_norm_rope, kv_cache_extend and kv_cache_release check
+// their tensors' shapes, types, strides and devices here, the others nothing beyond what the Python side checked.  The entry points come as addresses, so that this module
 // works with whichever build of the library the binding loaded.
 #include <Python.h>
 
@@ -34,6 +34,9 @@ struct Entries {
   decltype(&kv_cache_read_fp4) cache_read_fp4;
   decltype(&tree_commit_fp4) commit_fp4;
   decltype(&prompt_attention) prompt;
+  decltype(&tree_norm_rope) norm_rope;
+  decltype(&kv_cache_extend) cache_extend;
+  decltype(&kv_cache_release) cache_release;
 } lib;
 PyObject *check_call, *get_device, *raw_stream;
 
@@ -434,6 +437,9 @@ PyObject* commit_fp4(PyObject* const* a) {
   return tuple_of(rows[0], rows[1]);
 }
 
+// A tensor argument that may be None.
+const at::Tensor* optional(PyObject* o) { return o == Py_None ? nullptr : &tensor(o); }
+
 // Tokens of [tokens, heads, head_dim] that need not lie one behind the other.
 int64_t token_stride(const at::Tensor& t, const char* what) {
   three_dims(t);
@@ -487,8 +493,112 @@ PyObject* prompt(PyObject* const* a) {  // ctx, q, k, v, cu_tokens, scale, out, 
   return lse.defined() ? tuple_of(out, lse) : wrap(out);
 }
 
-// A tensor argument that may be None.
-const at::Tensor* optional(PyObject* o) { return o == Py_None ? nullptr : &tensor(o); }
+
+// ctx, position, q, k, q_weight, k_weight (or None), eps, base, rotary_dim (or None), pairing, q_out, k_out (or None)
+PyObject* norm_rope(PyObject* const* a) {
+  auto ctx = pointer<smart_ctx>(a[0]);
+  const at::Tensor &position = tensor(a[1]), &q = tensor(a[2]), &k = tensor(a[3]);
+  norm_rope_params p = {};
+  p.q_stride = token_stride(q, "q");
+  p.k_stride = token_stride(k, "k");
+  if (k.scalar_type() != q.scalar_type() || k.size(0) != q.size(0) || k.size(2) != q.size(2)) {
+    PyErr_SetString(PyExc_ValueError, "tree_norm_rope: q [N, Hq, D] and k [N, Hkv, D] of one element type");
+    throw Failed();
+  }
+  p.dtype = element_type(q);
+  p.n_tokens = extent32(q.size(0));
+  p.num_q_heads = extent32(q.size(1));
+  p.num_kv_heads = extent32(k.size(1));
+  p.head_dim = extent32(q.size(2));
+  elements(position, at::kInt, q.size(0), "position");
+  one_device({&q, &k, &position});
+  const at::Tensor* weights[] = {optional(a[4]), optional(a[5])};
+  for (const at::Tensor* w : weights)
+    if (w) {
+      elements(*w, q.scalar_type(), q.size(2), "q_weight, k_weight");
+      one_device({&q, w});
+    }
+  p.eps = (float)real(a[6]);
+  p.base = real(a[7]);
+  p.rotary_dim = a[8] == Py_None ? p.head_dim : (int32_t)integer(a[8]);
+  p.pairing = (int32_t)integer(a[9]);
+  at::Tensor q_out = a[10] == Py_None ? fresh(q, q.scalar_type(), q.sizes()) : tensor(a[10]);
+  at::Tensor k_out = a[11] == Py_None ? fresh(k, k.scalar_type(), k.sizes()) : tensor(a[11]);
+  same_shape(q, q_out, "q_out");
+  same_shape(k, k_out, "k_out");
+  p.q_out_stride = token_stride(q_out, "q_out");
+  p.k_out_stride = token_stride(k_out, "k_out");
+  p.d_position = address<int32_t>(position);
+  p.d_q = address(q);
+  p.d_k = address(k);
+  p.d_q_weight = weights[0] ? address(*weights[0]) : nullptr;
+  p.d_k_weight = weights[1] ? address(*weights[1]) : nullptr;
+  p.d_q_out = address(q_out);
+  p.d_k_out = address(k_out);
+  void* s = stream(&q);
+  call("tree_norm_rope", [&] { return lib.norm_rope(ctx, s, &p); });
+  return tuple_of(q_out, k_out);
+}
+
+// What the calls on block tables take: numbers of the batch, [batch, blocks] tables, a list of free blocks and its count.
+int32_t block_tensors(std::initializer_list<const at::Tensor*> numbers, const at::Tensor& table, const at::Tensor& free, const at::Tensor& count) {
+  const at::Tensor& first = **numbers.begin();
+  const int64_t batch = extent(first, 0);
+  for (const at::Tensor* t : numbers) {
+    elements(*t, at::kInt, batch, "numbers of the sequences");
+    one_device({&first, t});
+  }
+  elements(table, at::kInt, batch * extent(table, 1), "block_table");
+  elements(free, at::kInt, 0, "free_blocks");
+  elements(count, at::kInt, 1, "free_count");
+  one_device({&first, &table, &free, &count});
+  return extent32(batch);
+}
+
+// ctx, length, new_tokens, held, block_table, free_blocks, free_count, block_size, num_blocks, total_cap
+PyObject* cache_extend(PyObject* const* a) {
+  auto ctx = pointer<smart_ctx>(a[0]);
+  const at::Tensor &length = tensor(a[1]), &more = tensor(a[2]), &held = tensor(a[3]), &table = tensor(a[4]), &free = tensor(a[5]),
+                   &count = tensor(a[6]);
+  const int32_t batch = block_tensors({&length, &more, &held}, table, free, count), blocks = extent32(table.size(1)), bs = extent32(integer(a[7])),
+                num_blocks = extent32(integer(a[8])), cap = extent32(integer(a[9])), free_cap = extent32(free.numel());
+  if (cap < 0) {
+    PyErr_SetString(PyExc_ValueError, "kv_cache_extend: total_cap is negative");
+    throw Failed();
+  }
+  auto rows = i32_rows(4, std::max<int64_t>(batch, 1), length);  // (one number in the last)
+  at::Tensor cu = fresh(length, at::kInt, {batch + 1}), slots = fresh(length, at::kLong, {cap}), new_count = rows[3].slice(0, 0, 1);
+  for (int i = 0; i < 3; ++i) rows[i] = rows[i].slice(0, 0, batch);
+  void* s = stream(&length);
+  call("kv_cache_extend", [&] {
+    return lib.cache_extend(ctx, s, batch, bs, blocks, num_blocks, address<int32_t>(length), address<int32_t>(more), address<int32_t>(held),
+                            address<int32_t>(free), free_cap, address<int32_t>(count), address<int32_t>(table), cap, address<int32_t>(cu),
+                            address<int64_t>(slots), address<int32_t>(rows[0]), address<int32_t>(rows[1]), address<int32_t>(new_count),
+                            address<int32_t>(rows[2]));
+  });
+  return tuple_of(cu, slots, rows[0], rows[1], new_count, rows[2]);
+}
+
+// ctx, length, held, released, block_table, free_blocks, free_count, block_size, finished (or None), window, sinks
+PyObject* cache_release(PyObject* const* a) {
+  auto ctx = pointer<smart_ctx>(a[0]);
+  const at::Tensor &length = tensor(a[1]), &held = tensor(a[2]), &released = tensor(a[3]), &table = tensor(a[4]), &free = tensor(a[5]),
+                   &count = tensor(a[6]), *finished = optional(a[8]);
+  const int32_t batch = block_tensors({&length, &held, &released, finished ? finished : &length}, table, free, count),
+                blocks = extent32(table.size(1)), bs = extent32(integer(a[7])), window = extent32(integer(a[9])), sinks = extent32(integer(a[10])),
+                free_cap = extent32(free.numel());
+  auto rows = i32_rows(5, std::max<int64_t>(batch, 1), length);
+  at::Tensor new_count = rows[4].slice(0, 0, 1);
+  for (int i = 0; i < 4; ++i) rows[i] = rows[i].slice(0, 0, batch);
+  void* s = stream(&length);
+  call("kv_cache_release", [&] {
+    return lib.cache_release(ctx, s, batch, bs, blocks, window, sinks, address<int32_t>(length), address<int32_t>(held), address<int32_t>(released),
+                             finished ? address<int32_t>(*finished) : nullptr, address<int32_t>(table), address<int32_t>(free), free_cap,
+                             address<int32_t>(count), address<int32_t>(rows[0]), address<int32_t>(rows[1]), address<int32_t>(rows[2]),
+                             address<int32_t>(new_count), address<int32_t>(rows[3]));
+  });
+  return tuple_of(rows[0], rows[1], rows[2], new_count, rows[3]);
+}
 
 // What attention over a 4-bit cache needs of its tensors beside the caches' pages (page_bytes), for the arguments below.
 void attention_tensors(PyObject* const* a) {
@@ -674,6 +784,7 @@ PyMethodDef methods[] = {SMART_METHOD(setup, 4),       SMART_METHOD(select_begin
                          SMART_METHOD(accept, 6),      SMART_METHOD(sample, 8),     SMART_METHOD(commit, 18),
                          SMART_METHOD(attention_fp4, 21), SMART_METHOD(cache_write_fp4, 7), SMART_METHOD(cache_read_fp4, 7),
                          SMART_METHOD(commit_fp4, 11), SMART_METHOD(prompt, 9),
+                         SMART_METHOD(norm_rope, 12), SMART_METHOD(cache_extend, 10), SMART_METHOD(cache_release, 11),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef marshal_module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
