@@ -31,6 +31,9 @@
  *                          advances the prefix lengths (closes the step's loop)
  *   prompt_attention       causal attention of whole prompts (the prefill whose
  *                          K/V rows become the cached prefix)
+ *   prompt_attention_window
+ *                          the same where a token sees a sliding window and the
+ *                          first few tokens
  *   tree_norm_rope         norms each head of queries and keys and rotates it
  *   kv_cache_extend,       block tables and slot maps from request lengths, and
  *   kv_cache_release       pages back to the list of free ones
@@ -861,6 +864,11 @@ typedef struct {
 } prompt_params;
 
 int32_t prompt_attention(smart_ctx* ctx, void* stream, const prompt_params* params);
+
+/* prompt_attention with a sliding window: token t of a prompt sees the tokens u <= t with t - u < window (itself among
+ * them) or u < sinks, counted from the prompt's first token; nothing that another token holds enters its row.  Everything
+ * else, lse and errors included, as prompt_attention; SMART_EINVAL also for window < 1 or sinks < 0. */
+int32_t prompt_attention_window(smart_ctx* ctx, void* stream, const prompt_params* params, int32_t window, int32_t sinks);
 
 /* ---------------------------------------------------------------------------
  * tree_norm_rope (device)

@@ -2,14 +2,20 @@
 
     out[t, h] = sum_{u <= t, same prompt} softmax_u(scale <q[t, h], k[u, h // G]>) v[u, h // G]
 
-written row by row over the row's own keys, so that nothing else enters it.
+written row by row over the row's own keys, so that nothing else enters it.  With a window the keys are those u <= t with
+t - u < window or u < sinks.
 """
 from __future__ import annotations
 
 import numpy as np
 
 
-def prompt_attention(q, k, v, cu, scale):
+def seen(t, window, sinks):
+    """The tokens that token t of a prompt sees, ascending."""
+    return [u for u in range(t + 1) if window is None or t - u < window or u < sinks]
+
+
+def prompt_attention(q, k, v, cu, scale, window=None, sinks=0):
     """q [T, Hq, D], k, v [T, Hkv, D] float64; returns out, lse [T, Hq], and per element the softmax average of |v| and per
     row the largest sum |q| |k| (what error bounds are made of).  Rows of no prompt stay NaN."""
     T, Hq, D = q.shape
@@ -19,8 +25,8 @@ def prompt_attention(q, k, v, cu, scale):
     for lo, hi in zip(cu[:-1], cu[1:]):
         for t in range(lo, hi):
             for h in range(Hq):
-                out[t, h], lse[t, h], mean_abs[t, h], size[t, h] = prompt_row(q[t, h], k[lo:t + 1, h // G], v[lo:t + 1, h // G],
-                                                                              scale)
+                own = slice(lo, t + 1) if window is None else lo + np.array(seen(t - lo, window, sinks))
+                out[t, h], lse[t, h], mean_abs[t, h], size[t, h] = prompt_row(q[t, h], k[own, h // G], v[own, h // G], scale)
     return out, lse, mean_abs, size
 
 

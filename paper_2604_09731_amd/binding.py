@@ -36,7 +36,7 @@ EXPORTS = ["smart_strerror", "smart_last_hip_error", "smart_create", "smart_dest
            "tree_upload_pack", "tree_pack",
            "kv_cache_write", "kv_cache_write_fp8", "tree_verify_attention", "tree_verify_attention_static", "tree_accept", "tree_accept_sample", "tree_commit", "tree_commit_fp8",
            "kv_cache_write_fp4", "kv_cache_read_fp4", "tree_commit_fp4", "prompt_attention",
-           "tree_norm_rope", "kv_cache_extend", "kv_cache_release"]
+           "tree_norm_rope", "kv_cache_extend", "kv_cache_release", "prompt_attention_window"]
 
 
 class SmartError(RuntimeError):
@@ -192,6 +192,8 @@ def _lib():
                                         vp, vp, i64, i64, vp, vp]
         lib.prompt_attention.restype = i32
         lib.prompt_attention.argtypes = [vp, vp, ctypes.POINTER(PromptParams)]
+        lib.prompt_attention_window.restype = i32
+        lib.prompt_attention_window.argtypes = [vp, vp, ctypes.POINTER(PromptParams), i32, i32]
         lib.tree_norm_rope.restype = i32
         lib.tree_norm_rope.argtypes = [vp, vp, ctypes.POINTER(NormRopeParams)]
         lib.kv_cache_extend.restype = i32
@@ -431,7 +433,7 @@ _NATIVE_ENTRIES = ("smart_select_begin_device", "smart_select_layer_device", "tr
                    "tree_rope", "kv_cache_write", "kv_cache_write_fp8", "tree_verify_attention",
                    "tree_verify_attention_static", "tree_accept", "tree_accept_sample", "tree_commit", "tree_commit_fp8",
                    "kv_cache_write_fp4", "kv_cache_read_fp4", "tree_commit_fp4", "prompt_attention",
-                   "tree_norm_rope", "kv_cache_extend", "kv_cache_release")
+                   "tree_norm_rope", "kv_cache_extend", "kv_cache_release", "prompt_attention_window")
 _nativeh = None
 
 
@@ -648,11 +650,16 @@ class SmartTree:
         return k_out, v_out
 
     # -- prompt_attention --------------------------------------------------
-    def prompt_attention(self, q, k, v, cu_tokens, softmax_scale, out=None, lse=None, want_lse=False):
+    def prompt_attention(self, q, k, v, cu_tokens, softmax_scale, out=None, lse=None, want_lse=False, window=None, sinks=0):
         """Causal attention of packed prompts: q [T, Hq, D], k and v [T, Hkv, D] (tokens may be strided, as parts of one
         projection's output are), prompt b the tokens cu_tokens[b] .. cu_tokens[b + 1] - 1.  Returns out (like q,
-        contiguous unless given), or (out, lse [T, Hq]) if lse is given or wanted; rows of no prompt are not written."""
+        contiguous unless given), or (out, lse [T, Hq]) if lse is given or wanted; rows of no prompt are not written.
+        ``window``: a token sees the last ``window`` tokens of its prompt only, its own among them, and the first ``sinks``."""
         self._here(q)
+        if window is not None:
+            return self._native.prompt_window(self._ctx, q, k, v, cu_tokens, softmax_scale, out, lse, want_lse, window, sinks)
+        if sinks:
+            raise ValueError("sinks without a window")
         return self._native.prompt(self._ctx, q, k, v, cu_tokens, softmax_scale, out, lse, want_lse)
 
     # -- tree_verify_attention ---------------------------------------------

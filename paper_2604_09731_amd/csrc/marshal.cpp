@@ -37,6 +37,7 @@ struct Entries {
   decltype(&tree_norm_rope) norm_rope;
   decltype(&kv_cache_extend) cache_extend;
   decltype(&kv_cache_release) cache_release;
+  decltype(&prompt_attention_window) prompt_window;
 } lib;
 PyObject *check_call, *get_device, *raw_stream;
 
@@ -70,6 +71,12 @@ uint64_t low_bits(PyObject* n) {  // of an int, whose reference it takes
 uint64_t bits64(PyObject* o) { return low_bits(PyNumber_Long(o)); }  // what int(o) gives, modulo 2^64
 // An integer; anything else, a float of a whole value among them, is refused as ctypes refuses it.
 int64_t integer(PyObject* o) { return (int64_t)low_bits(PyNumber_Index(o)); }
+int32_t integer32(PyObject* o) {
+  const int64_t n = integer(o);
+  if (n >= INT32_MIN && n <= INT32_MAX) return (int32_t)n;
+  PyErr_SetString(PyExc_ValueError, "an integer does not fit 32 bits");
+  throw Failed();
+}
 bool truth(PyObject* o) {
   const int v = PyObject_IsTrue(o);
   if (v < 0) throw Failed();
@@ -451,7 +458,9 @@ int64_t token_stride(const at::Tensor& t, const char* what) {
   return t.size(0) > 1 ? t.stride(0) : t.size(1) * t.size(2);
 }
 
-PyObject* prompt(PyObject* const* a) {  // ctx, q, k, v, cu_tokens, scale, out, lse, want_lse
+// ctx, q, k, v, cu_tokens, scale, out, lse, want_lse (, window, sinks)
+template <bool kWindow>
+PyObject* prompt_over(PyObject* const* a) {
   auto ctx = pointer<smart_ctx>(a[0]);
   const at::Tensor &q = tensor(a[1]), &k = tensor(a[2]), &v = tensor(a[3]), &cu = tensor(a[4]);
   prompt_params p = {};
@@ -488,10 +497,14 @@ PyObject* prompt(PyObject* const* a) {  // ctx, q, k, v, cu_tokens, scale, out, 
   p.d_cu_tokens = address<int32_t>(cu);
   p.d_out = address(out);
   p.d_lse = lse.defined() ? address<float>(lse) : nullptr;
+  const int32_t window = kWindow ? integer32(a[9]) : 0, sinks = kWindow ? integer32(a[10]) : 0;
   void* s = stream(&q);
-  call("prompt_attention", [&] { return lib.prompt(ctx, s, &p); });
+  if (kWindow) call("prompt_attention_window", [&] { return lib.prompt_window(ctx, s, &p, window, sinks); });
+  else call("prompt_attention", [&] { return lib.prompt(ctx, s, &p); });
   return lse.defined() ? tuple_of(out, lse) : wrap(out);
 }
+PyObject* prompt(PyObject* const* a) { return prompt_over<false>(a); }
+PyObject* prompt_window(PyObject* const* a) { return prompt_over<true>(a); }
 
 
 // ctx, position, q, k, q_weight, k_weight (or None), eps, base, rotary_dim (or None), pairing, q_out, k_out (or None)
@@ -520,8 +533,8 @@ PyObject* norm_rope(PyObject* const* a) {
     }
   p.eps = (float)real(a[6]);
   p.base = real(a[7]);
-  p.rotary_dim = a[8] == Py_None ? p.head_dim : (int32_t)integer(a[8]);
-  p.pairing = (int32_t)integer(a[9]);
+  p.rotary_dim = a[8] == Py_None ? p.head_dim : integer32(a[8]);
+  p.pairing = integer32(a[9]);
   at::Tensor q_out = a[10] == Py_None ? fresh(q, q.scalar_type(), q.sizes()) : tensor(a[10]);
   at::Tensor k_out = a[11] == Py_None ? fresh(k, k.scalar_type(), k.sizes()) : tensor(a[11]);
   same_shape(q, q_out, "q_out");
@@ -560,8 +573,8 @@ PyObject* cache_extend(PyObject* const* a) {
   auto ctx = pointer<smart_ctx>(a[0]);
   const at::Tensor &length = tensor(a[1]), &more = tensor(a[2]), &held = tensor(a[3]), &table = tensor(a[4]), &free = tensor(a[5]),
                    &count = tensor(a[6]);
-  const int32_t batch = block_tensors({&length, &more, &held}, table, free, count), blocks = extent32(table.size(1)), bs = extent32(integer(a[7])),
-                num_blocks = extent32(integer(a[8])), cap = extent32(integer(a[9])), free_cap = extent32(free.numel());
+  const int32_t batch = block_tensors({&length, &more, &held}, table, free, count), blocks = extent32(table.size(1)), bs = integer32(a[7]),
+                num_blocks = integer32(a[8]), cap = integer32(a[9]), free_cap = extent32(free.numel());
   if (cap < 0) {
     PyErr_SetString(PyExc_ValueError, "kv_cache_extend: total_cap is negative");
     throw Failed();
@@ -585,7 +598,7 @@ PyObject* cache_release(PyObject* const* a) {
   const at::Tensor &length = tensor(a[1]), &held = tensor(a[2]), &released = tensor(a[3]), &table = tensor(a[4]), &free = tensor(a[5]),
                    &count = tensor(a[6]), *finished = optional(a[8]);
   const int32_t batch = block_tensors({&length, &held, &released, finished ? finished : &length}, table, free, count),
-                blocks = extent32(table.size(1)), bs = extent32(integer(a[7])), window = extent32(integer(a[9])), sinks = extent32(integer(a[10])),
+                blocks = extent32(table.size(1)), bs = integer32(a[7]), window = integer32(a[9]), sinks = integer32(a[10]),
                 free_cap = extent32(free.numel());
   auto rows = i32_rows(5, std::max<int64_t>(batch, 1), length);
   at::Tensor new_count = rows[4].slice(0, 0, 1);
@@ -785,6 +798,7 @@ PyMethodDef methods[] = {SMART_METHOD(setup, 4),       SMART_METHOD(select_begin
                          SMART_METHOD(attention_fp4, 21), SMART_METHOD(cache_write_fp4, 7), SMART_METHOD(cache_read_fp4, 7),
                          SMART_METHOD(commit_fp4, 11), SMART_METHOD(prompt, 9),
                          SMART_METHOD(norm_rope, 12), SMART_METHOD(cache_extend, 10), SMART_METHOD(cache_release, 11),
+                         SMART_METHOD(prompt_window, 11),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef marshal_module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

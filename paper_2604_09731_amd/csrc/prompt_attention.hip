@@ -8,6 +8,8 @@
 //     probabilities come out in the operand layout of the second product.
 //   * Row tiles are handed out from the longest down, of up to 64 prompts: what is dispatched last is short.
 //   * Bound by the matrix cores: 4 D flops per (row, key).
+//   * With a window (prompt_attention_window) a row tile streams the first tokens that stay visible and what the windows of its rows
+//     hold, as one axis without the gap between them (Span); every variant is compiled for both.
 //   * Values of later tokens are multiplied by probabilities of zero where a tile crosses the diagonal; a row that comes out
 //     infinite or NaN is evaluated once more over its own keys only (evaluate_again).
 #include <math.h>
@@ -45,6 +47,7 @@ struct PromptArgs {
   const int32_t* cu;
   int64_t q_stride, k_stride, v_stride, out_stride;
   int32_t batch, total_tokens, Hq, Hkv, G;
+  int32_t window, sinks;  // (at most total_tokens each)
   uint32_t num_cus;
   float scale, c;  // c: in powers of two
 };
@@ -141,6 +144,27 @@ __device__ inline Item find_item(const PromptArgs& a, int rank) {
   return s_item;
 }
 
+// The keys that rows of tokens first .. need, numbered without the gap between the first tokens, which all see, and the first one's
+// window: key v is token v, or v + shift from the gap on.  A row of token t, which is key t - shift, sees the keys up to its own
+// that are no more than a window behind it or among the first `sinks`.  A stage with keys from both sides of the gap is addressed
+// from the prompt's first token; where 32 bits do not reach that far the gap begins with a stage (the keys before it are hidden).
+template <bool kWindow>
+struct Span {
+  int shift = 0, gap = 0, sinks = 0, window = 0;
+  __device__ Span(const PromptArgs& a, int first, int len) {
+    if (!kWindow) return;
+    const int begin = first - a.window + 1;
+    const bool reaches = max(a.k_stride, a.v_stride) * len < (int64_t)1 << 30;
+    sinks = a.sinks;
+    window = a.window;
+    const int until = reaches ? sinks : (sinks + 63) & ~63;
+    if (begin > until) shift = begin - until, gap = until;
+  }
+  __device__ int token(int v) const { return kWindow && v >= gap ? v + shift : v; }
+  // key: of the row itself
+  __device__ bool hidden(int v, int key) const { return v > key || (kWindow && v >= sinks && v <= key - window); }
+};
+
 // ---- staging: global memory -> registers -> LDS, in 16-byte chunks of rows ----------------------------------------------
 // Chunk c of row `key` lies at position c ^ swizzle(key), so that the reads of both products (a row per lane; four rows of
 // sixteen elements per sixteen lanes) are free of bank conflicts.  (Bit 2 of the key takes no part: rows four apart are read by
@@ -172,10 +196,29 @@ struct Stage {
       vo[i] = ((uint32_t)row * (uint32_t)a.v_stride + c * kE) * (uint32_t)sizeof(T);
     }
   }
+  // The same of a stage with tokens from both sides of a window's gap, from the prompt's first token.
+  __device__ void place_both(const PromptArgs& a, const Span<true>& span, int key0, int len, int tid) {
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const int p = i * kThreads + tid, key = p / kRowChunks, c = (p % kRowChunks) ^ swizzle<T, D>(key);
+      const int row = min(span.token(key0 + key), len - 1);
+      ko[i] = ((uint32_t)row * (uint32_t)a.k_stride + c * kE) * (uint32_t)sizeof(T);
+      vo[i] = ((uint32_t)row * (uint32_t)a.v_stride + c * kE) * (uint32_t)sizeof(T);
+    }
+  }
   // Stages are requested in order; the last one may be short.
-  __device__ void load(const T* kp, const T* vp, const PromptArgs& a, int key0, int len, int tid) {
-    if (key0 == 0 || key0 + kKeys > len) place(a, len - key0, tid);
-    const char *kb = (const char*)(kp + key0 * a.k_stride), *vb = (const char*)(vp + key0 * a.v_stride);
+  template <bool kWindow>
+  __device__ void load(const T* kp, const T* vp, const PromptArgs& a, const Span<kWindow>& span, int key0, int len, int tid) {
+    int token0 = key0;
+    if constexpr (kWindow) {
+      const bool both = key0 < span.gap && key0 + kKeys > span.gap;
+      token0 = both ? 0 : span.token(key0);
+      if (both) place_both(a, span, key0, len, tid);
+      else if (key0 == 0 || key0 - kKeys < span.gap || token0 + kKeys > len) place(a, len - token0, tid);
+    } else {
+      if (key0 == 0 || key0 + kKeys > len) place(a, len - key0, tid);
+    }
+    const char *kb = (const char*)(kp + token0 * a.k_stride), *vb = (const char*)(vp + token0 * a.v_stride);
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
       k[i] = *(const uintx4*)(kb + ko[i]);
@@ -203,11 +246,13 @@ __device__ inline void put_four(__bf16* p, floatx4 x) { *(bf16x4*)p = __builtin_
 // Rows that are infinite or NaN by their own keys come here too.  So one bad value of an early token sends every later row of its kv
 // head here, and this has to be of the order of the call itself: with an infinity in the first token of all kv heads 3000 tokens of
 // 16 / 4 heads take 575 us instead of 73 (bf16, head dim 128), 309 instead of 46 (64), 476 instead of 200 (fp32, 64).
-template <typename T, int D>
+template <typename T, int D, bool kWindow>
 __device__ void evaluate_again(const PromptArgs& a, int base, int g, int mine, int rows, uint32_t which, int lane) {
   asm volatile("" : "+v"(lane));  // (everything is derived anew, so that nothing lives in registers until here)
   const int w = lane >> 4, i = lane & 15;
-  const int rho = min(mine + i, rows - 1), token = rho / a.G, head = g * a.G + rho % a.G, last = (min(mine + 16, rows) - 1) / a.G;
+  const int rho = min(mine + i, rows - 1), token = rho / a.G, head = g * a.G + rho % a.G;
+  const Span<kWindow> span(a, mine / a.G, rows / a.G);
+  const int last = (min(mine + 16, rows) - 1) / a.G - span.shift, own = token - span.shift;
   const T* qp = (const T*)a.q + (int64_t)(base + token) * a.q_stride + (int64_t)head * D + 4 * w;
   const T* kp = (const T*)a.k + (int64_t)base * a.k_stride + (int64_t)g * D + 4 * w;
   const T* vp = (const T*)a.v + (int64_t)base * a.v_stride + (int64_t)g * D + 4 * i;
@@ -224,8 +269,8 @@ __device__ void evaluate_again(const PromptArgs& a, int base, int g, int mine, i
 #pragma unroll
     for (int r = 0; r < 4; ++r)
 #pragma unroll
-      for (int x = 0; x < D / 64; ++x) v[r][x] = four(vp + min(key0 + 4 * w + r, last) * a.v_stride + 64 * x);
-    const T* kr = kp + min(key0 + i, last) * a.k_stride;
+      for (int x = 0; x < D / 64; ++x) v[r][x] = four(vp + span.token(min(key0 + 4 * w + r, last)) * a.v_stride + 64 * x);
+    const T* kr = kp + span.token(min(key0 + i, last)) * a.k_stride;
 #pragma unroll
     for (int x = 0; x < D / 16; ++x) {
       const floatx4 k = four(kr + 16 * x);
@@ -234,7 +279,7 @@ __device__ void evaluate_again(const PromptArgs& a, int base, int g, int mine, i
     }
 #pragma unroll
     for (int r = 0; r < 4; ++r)
-      if (key0 + 4 * w + r > token) s[r] = -INFINITY;
+      if (span.hidden(key0 + 4 * w + r, own)) s[r] = -INFINITY;
     const float now = fmaxf(m, max_quarters(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]))));
     if (__any(now != m)) {
       const float alpha = now == m ? 1.f : exp2f((m - now) * a.c);
@@ -297,7 +342,7 @@ __device__ void evaluate_again(const PromptArgs& a, int base, int g, int mine, i
 // 6600 tokens of 8 prompts 103 us (102 TFLOP/s; with 32 x 32 tiles, 128 rows and no sharing 148; 64 rows without sharing 110), one
 // prompt of 1536 62 (129, 72), of 300 16.6 (29, 17.7), 4 of 4096 571 (653, 579); head dim 128, 4 of 2048 324 (335, 341).  Left without
 // the softmax it takes 6 % less, without staging 8 %; the rest is what the ends of the row tiles leave idle.
-template <int D>
+template <int D, bool kWindow>
 __global__ __launch_bounds__(512, D == 64 ? 4 : 2) void prompt_f32_kernel(PromptArgs a) {
   constexpr int kThreads = 512, kTileRows = 16, kRowWaves = kThreads / kWave / 2, kRows = kRowWaves * kTileRows;
   typedef Stage<float, D, kThreads> S;
@@ -310,9 +355,10 @@ __global__ __launch_bounds__(512, D == 64 ? 4 : 2) void prompt_f32_kernel(Prompt
   const int base = __builtin_amdgcn_readfirstlane(it.base), len = __builtin_amdgcn_readfirstlane(it.len);
   const int rows = len * a.G, row0 = __builtin_amdgcn_readfirstlane(it.tile) * kRows;
   const int mine = row0 + wv * kTileRows;                    // this wavefront's first row
-  const int keys = (min(row0 + kRows, rows) - 1) / a.G + 1;  // keys of the workgroup
-  const int last = (min(mine + kTileRows, rows) - 1) / a.G;  // the last key of the wavefront (with rows)
-  const int first = min(mine, rows - 1) / a.G;               // and its first token
+  const Span<kWindow> span(a, row0 / a.G, len);
+  const int keys = (min(row0 + kRows, rows) - 1) / a.G + 1 - span.shift;  // keys of the workgroup
+  const int last = (min(mine + kTileRows, rows) - 1) / a.G - span.shift;  // the last key of the wavefront (with rows)
+  const int first = min(mine, rows - 1) / a.G - span.shift;               // and its first row's own
 
   const int rho = min(mine + i16, rows - 1);  // padding rows repeat the last real row; never written
   const int token = rho / a.G, head = g * a.G + rho % a.G;
@@ -330,15 +376,16 @@ __global__ __launch_bounds__(512, D == 64 ? 4 : 2) void prompt_f32_kernel(Prompt
   const float* vp = (const float*)a.v + (int64_t)base * a.v_stride + (int64_t)g * D;
   const int steps = (keys + S::kKeys - 1) / S::kKeys;
   S stage;
-  stage.load(kp, vp, a, 0, len, tid);
+  stage.load(kp, vp, a, span, 0, len, tid);
   for (int t = 0; t < steps; ++t) {
     uintx4* at = lds[t & 1];
     stage.store(at, tid);
-    if (t + 1 < steps) stage.load(kp, vp, a, (t + 1) * S::kKeys, len, tid);
+    if (t + 1 < steps) stage.load(kp, vp, a, span, (t + 1) * S::kKeys, len, tid);
     __syncthreads();  // the stage is full, and everyone is done with the other one
     const int key0 = t * S::kKeys + 32 * part;
     const uintx4 *kt0 = at + 32 * part * S::kRowChunks, *vt = kt0 + S::kChunks;
     if (mine >= rows || key0 > last) continue;
+    if (kWindow && key0 >= span.sinks && key0 + 31 <= first - span.window) continue;
     floatx4 s[2];
     s[0] = s[1] = (floatx4)(0.f);
 #pragma unroll
@@ -352,10 +399,10 @@ __global__ __launch_bounds__(512, D == 64 ? 4 : 2) void prompt_f32_kernel(Prompt
 #pragma unroll
         for (int kt = 0; kt < 2; ++kt) s[kt] = __builtin_amdgcn_mfma_f32_16x16x4f32(k[kt][e], q[x][e], s[kt], 0, 0, 0);
     }
-    if (key0 + 31 > first) {
+    if (key0 + 31 > first || (kWindow && key0 + 31 >= span.sinks && key0 <= last - span.window)) {
 #pragma unroll
       for (int r = 0; r < 8; ++r)
-        if (key0 + 16 * (r >> 2) + 4 * w + (r & 3) > token) s[r >> 2][r & 3] = -INFINITY;
+        if (span.hidden(key0 + 16 * (r >> 2) + 4 * w + (r & 3), token - span.shift)) s[r >> 2][r & 3] = -INFINITY;
     }
     float mx = s[0][0];
 #pragma unroll
@@ -427,7 +474,7 @@ __global__ __launch_bounds__(512, D == 64 ? 4 : 2) void prompt_f32_kernel(Prompt
   if (a.lse && there && w == 0) a.lse[(int64_t)(base + token) * a.Hq + head] = sum == 0.f ? -INFINITY : m * a.scale + logf(sum);
   uint64_t again = __ballot(there && bad != 0.f && sum < INFINITY);
   again = (again | again >> 16 | again >> 32 | again >> 48) & 0xFFFFull;
-  if (again) evaluate_again<float, D>(a, base, g, mine, rows, (uint32_t)again, lane);
+  if (again) evaluate_again<float, D, kWindow>(a, base, g, mine, rows, (uint32_t)again, lane);
 }
 
 // ---- bf16 -----------------------------------------------------------------------------------------------------------------
@@ -441,7 +488,7 @@ typedef __attribute__((address_space(3))) uintx4 lds_uintx4;
 // A wavefront's 16 N rows: products of 16 x 16 tiles, 32 keys at a time.  Lane (quarter w, i): of a score tile, row i and four
 // keys; the two score tiles of a step are made of keys 8 w + 0 .. 3 and 8 w + 4 .. 7, so that a lane's eight probabilities are
 // the eight consecutive keys that it contributes to the output product.
-template <int D, int N, bool kLse>
+template <int D, int N, bool kLse, bool kWindow>
 struct RowsBf16 {
   bf16x8 q[N][D / 32];
   floatx4 o[N][D / 16];
@@ -498,12 +545,14 @@ struct RowsBf16 {
         for (int r = 0; r < N; ++r)
           s[r][half] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[ks][half], q[r][ks], ks == 0 ? (floatx4)(0.f) : s[r][half], 0, 0, 0);
   }
-  __device__ void mask(floatx4 (&s)[N][2], int key0, int lane) const {
+  __device__ void mask(floatx4 (&s)[N][2], const Span<kWindow>& span, int key0, int lane) const {
+    const int at = key0 + 8 * (lane >> 4);
 #pragma unroll
     for (int r = 0; r < N; ++r)
 #pragma unroll
       for (int e = 0; e < 8; ++e)
-        if (e > token[r] - key0 - 8 * (lane >> 4)) s[r][e >> 2][e & 3] = -INFINITY;
+        if (e > token[r] - span.shift - at || (kWindow && e >= span.sinks - at && e <= token[r] - span.shift - span.window - at))
+          s[r][e >> 2][e & 3] = -INFINITY;
   }
   // Scores -> probabilities as the output product takes them.  The values are requested between the exponentials: a wavefront
   // that asks for all of them at once waits until the LDS has taken the requests of all wavefronts.
@@ -603,14 +652,14 @@ struct RowsBf16 {
       all_again |= ((again | again >> 16) & 0xFFFFull) << (16 * r);
     }
     for (int r = 0; all_again; ++r, all_again >>= 16)
-      if (all_again & 0xFFFFull) evaluate_again<__bf16, D>(a, base, g, mine + 16 * r, rows, (uint32_t)(all_again & 0xFFFFull), lane);
+      if (all_again & 0xFFFFull) evaluate_again<__bf16, D, kWindow>(a, base, g, mine + 16 * r, rows, (uint32_t)(all_again & 0xFFFFull), lane);
   }
 };
 
 // A stage is 64 keys, two parts of 32.  Stage t lies in buffer t % 2.  It is written behind the barrier of stage t - 2, when nobody
 // reads that one any more, out of registers that were requested a stage earlier, and first read (the keys of its first part)
 // behind the barrier of stage t - 1.
-template <int D, int kWaves, int N, bool kLse>
+template <int D, int kWaves, int N, bool kLse, bool kWindow>
 __global__ __launch_bounds__(kWaves* kWave, D == 64 && N == 2 ? 3 : 2) void prompt_bf16_kernel(PromptArgs a) {
   constexpr int kThreads = kWaves * kWave, kMine = 16 * N, kRows = kWaves * kMine;
   typedef Stage<__bf16, D, kThreads> S;
@@ -629,22 +678,23 @@ __global__ __launch_bounds__(kWaves* kWave, D == 64 && N == 2 ? 3 : 2) void prom
   const int base = __builtin_amdgcn_readfirstlane(it.base), len = __builtin_amdgcn_readfirstlane(it.len);
   const int rows = len * a.G, row0 = __builtin_amdgcn_readfirstlane(it.tile) * kRows;
   const int mine = row0 + wv * kMine;                                       // this wavefront's first row
-  const int keys = (min(row0 + kRows, rows) - 1) / a.G + 1;                 // keys of the workgroup
-  const int last = mine < rows ? (min(mine + kMine, rows) - 1) / a.G : -1;  // the last key of the wavefront
-  const int first = min(mine, rows - 1) / a.G;                              // its first token
+  const Span<kWindow> span(a, row0 / a.G, len);
+  const int keys = (min(row0 + kRows, rows) - 1) / a.G + 1 - span.shift;                 // keys of the workgroup
+  const int last = mine < rows ? (min(mine + kMine, rows) - 1) / a.G - span.shift : -1;  // the last key of the wavefront
+  const int first = min(mine, rows - 1) / a.G - span.shift;                              // its first row's own
   const int steps = (keys + S::kKeys - 1) / S::kKeys;
 
   const __bf16* kp = (const __bf16*)a.k + (int64_t)base * a.k_stride + (int64_t)g * D;
   const __bf16* vp = (const __bf16*)a.v + (int64_t)base * a.v_stride + (int64_t)g * D;
   S stage;
-  stage.load(kp, vp, a, 0, len, tid);
-  RowsBf16<D, N, kLse> x;
+  stage.load(kp, vp, a, span, 0, len, tid);
+  RowsBf16<D, N, kLse, kWindow> x;
   x.begin(a, base, g, mine, rows, lane, S::kChunks * 16);
   stage.store(lds[0], tid);
   if (steps > 1) {
-    stage.load(kp, vp, a, S::kKeys, len, tid);
+    stage.load(kp, vp, a, span, S::kKeys, len, tid);
     stage.store(lds[1], tid);
-    if (steps > 2) stage.load(kp, vp, a, 2 * S::kKeys, len, tid);
+    if (steps > 2) stage.load(kp, vp, a, span, 2 * S::kKeys, len, tid);
   }
   __syncthreads();
 
@@ -654,7 +704,7 @@ __global__ __launch_bounds__(kWaves* kWave, D == 64 && N == 2 ? 3 : 2) void prom
   auto fill = [&]() {  // behind the barrier of stage t
     if (t + 2 < steps) {
       stage.store(lds[t & 1], tid);
-      if (t + 3 < steps) stage.load(kp, vp, a, (t + 3) * S::kKeys, len, tid);
+      if (t + 3 < steps) stage.load(kp, vp, a, span, (t + 3) * S::kKeys, len, tid);
     }
   };
   auto next_stage = [&]() {
@@ -667,6 +717,29 @@ __global__ __launch_bounds__(kWaves* kWave, D == 64 && N == 2 ? 3 : 2) void prom
   floatx4 s[N][2];
   x.read_keys(k, at, 0);
   x.scores(s, k);
+  // Stages of which some row sees part (with a window also none); wavefronts that are done keep the stages coming.
+  auto edge = [&](int until) {
+    while (t < until) {
+#pragma unroll
+      for (int part = 0; part < 2; ++part) {
+        const int key0 = t * S::kKeys + 32 * part;
+        const bool more = key0 <= last, seen = more && !(kWindow && key0 >= span.sinks && key0 + 31 <= first - span.window);
+        if (seen) {
+          x.mask(s, span, key0, lane);
+          x.softmax(pb, s, a.c, v, at, part);
+        }
+        if (part == 1) {
+          __syncthreads();
+          fill();
+        }
+        if (seen) x.output(v, pb, k, part == 0 ? at : other, 1 - part);
+        else if (kWindow && more) x.read_keys(k, part == 0 ? at : other, 1 - part);
+        if (more) x.scores(s, k);
+      }
+      next_stage();
+    }
+  };
+  if (kWindow) edge(min(steps, last >= span.window ? (last - span.window) / S::kKeys + 1 : 0));  // where the windows begin
   // Stages that all rows of the wavefront see whole.
   const int whole = mine < rows ? (first + 1) / S::kKeys : 0;
   while (t < whole) {
@@ -685,26 +758,7 @@ __global__ __launch_bounds__(kWaves* kWave, D == 64 && N == 2 ? 3 : 2) void prom
     }
     next_stage();
   }
-  // the diagonal and the prompt's end; wavefronts that are done keep the stages coming
-  while (t < steps) {
-#pragma unroll
-    for (int part = 0; part < 2; ++part) {
-      const int key0 = t * S::kKeys + 32 * part;
-      if (key0 <= last) {
-        x.mask(s, key0, lane);
-        x.softmax(pb, s, a.c, v, at, part);
-      }
-      if (part == 1) {
-        __syncthreads();
-        fill();
-      }
-      if (key0 <= last) {
-        x.output(v, pb, k, part == 0 ? at : other, 1 - part);
-        x.scores(s, k);
-      }
-    }
-    next_stage();
-  }
+  edge(steps);  // the diagonal and the prompt's end
   if (mine < rows) x.finish(a, base, g, mine, rows, lane);
 }
 
@@ -718,10 +772,10 @@ int32_t launch(Kernel kernel, int threads, int rows, const PromptArgs& a, hipStr
   return SMART_OK;
 }
 
-template <int D, int kWaves, int N>
+template <int D, int kWaves, int N, bool kWindow>
 int32_t launch_rows(const PromptArgs& a, hipStream_t stream) {
-  return a.lse ? launch(prompt_bf16_kernel<D, kWaves, N, true>, kWaves * kWave, kWaves * 16 * N, a, stream)
-               : launch(prompt_bf16_kernel<D, kWaves, N, false>, kWaves * kWave, kWaves * 16 * N, a, stream);
+  return a.lse ? launch(prompt_bf16_kernel<D, kWaves, N, true, kWindow>, kWaves * kWave, kWaves * 16 * N, a, stream)
+               : launch(prompt_bf16_kernel<D, kWaves, N, false, kWindow>, kWaves * kWave, kWaves * 16 * N, a, stream);
 }
 
 // Taller row tiles read the LDS less often per product, but there have to be enough of them to fill the chip and to let the short
@@ -737,11 +791,18 @@ int tile_rows(const PromptArgs& a, bool f32) {
 }
 int tile_threads(int rows, bool f32, int D) { return f32 || (rows == 256 && D == 128) ? 512 : 256; }
 
-template <int D>
+template <int D, bool kWindow>
 int32_t launch_bf16(const PromptArgs& a, int rows, hipStream_t stream) {
-  if (rows == 64) return launch_rows<D, 4, 1>(a, stream);
-  if (rows == 128) return launch_rows<D, 4, 2>(a, stream);
-  return launch_rows<D, D == 128 ? 8 : 4, D == 128 ? 2 : 4>(a, stream);
+  if (rows == 64) return launch_rows<D, 4, 1, kWindow>(a, stream);
+  if (rows == 128) return launch_rows<D, 4, 2, kWindow>(a, stream);
+  return launch_rows<D, D == 128 ? 8 : 4, D == 128 ? 2 : 4, kWindow>(a, stream);
+}
+
+template <bool kWindow>
+int32_t launch_any(const PromptArgs& a, bool f32, int D, int rows, int threads, hipStream_t stream) {
+  if (f32)
+    return D == 128 ? launch(prompt_f32_kernel<128, kWindow>, threads, rows, a, stream) : launch(prompt_f32_kernel<64, kWindow>, threads, rows, a, stream);
+  return D == 128 ? launch_bf16<128, kWindow>(a, rows, stream) : launch_bf16<64, kWindow>(a, rows, stream);
 }
 
 int32_t check(const prompt_params& p) {
@@ -762,11 +823,8 @@ int32_t check(const prompt_params& p) {
   return SMART_OK;
 }
 
-}  // namespace
-
-extern "C" int32_t prompt_attention(smart_ctx* ctx, void* stream, const prompt_params* params) {
-  if (!ctx || !params) return SMART_EINVAL;
-  const prompt_params& p = *params;
+// window 0: none
+int32_t prompt(smart_ctx* ctx, void* stream, const prompt_params& p, int32_t window, int32_t sinks) {
   int32_t rc = check(p);
   if (rc != SMART_OK || p.batch == 0 || p.total_tokens == 0) return rc;
   PromptArgs a;
@@ -785,6 +843,8 @@ extern "C" int32_t prompt_attention(smart_ctx* ctx, void* stream, const prompt_p
   a.Hq = p.num_q_heads;
   a.Hkv = p.num_kv_heads;
   a.G = p.num_q_heads / p.num_kv_heads;
+  a.window = window < p.total_tokens ? window : p.total_tokens;
+  a.sinks = sinks < p.total_tokens ? sinks : p.total_tokens;
   a.num_cus = ctx->num_cus > 0 ? ctx->num_cus : 256;
   a.scale = p.softmax_scale;
   a.c = p.softmax_scale * kLog2e;
@@ -795,11 +855,21 @@ extern "C" int32_t prompt_attention(smart_ctx* ctx, void* stream, const prompt_p
   SMART_HIP_CHECK(hipGetDevice(&prev));
   if (prev != ctx->device) SMART_HIP_CHECK(hipSetDevice(ctx->device));
   hipStream_t s = (hipStream_t)stream;
-  if (f32) {
-    rc = p.head_dim == 128 ? launch(prompt_f32_kernel<128>, threads, rows, a, s) : launch(prompt_f32_kernel<64>, threads, rows, a, s);
-  } else {
-    rc = p.head_dim == 128 ? launch_bf16<128>(a, rows, s) : launch_bf16<64>(a, rows, s);
-  }
+  // (a window that no prompt can fill hides nothing)
+  rc = window > 0 && window < p.total_tokens ? launch_any<true>(a, f32, p.head_dim, rows, threads, s)
+                                             : launch_any<false>(a, f32, p.head_dim, rows, threads, s);
   if (prev != ctx->device) (void)hipSetDevice(prev);
   return rc;
+}
+
+}  // namespace
+
+extern "C" int32_t prompt_attention(smart_ctx* ctx, void* stream, const prompt_params* params) {
+  if (!ctx || !params) return SMART_EINVAL;
+  return prompt(ctx, stream, *params, 0, 0);
+}
+
+extern "C" int32_t prompt_attention_window(smart_ctx* ctx, void* stream, const prompt_params* params, int32_t window, int32_t sinks) {
+  if (!ctx || !params || window < 1 || sinks < 0) return SMART_EINVAL;
+  return prompt(ctx, stream, *params, window, sinks);
 }
