@@ -31,9 +31,9 @@
  *                          advances the prefix lengths (closes the step's loop)
  *   prompt_attention       causal attention of whole prompts (the prefill whose
  *                          K/V rows become the cached prefix)
- *   prompt_attention_window
- *                          the same where a token sees a sliding window and the
- *                          first few tokens
+ *   prompt_attention_window, tree_verify_attention_window
+ *                          the same where a token or node sees a sliding window
+ *                          and the first few tokens
  *   tree_norm_rope         norms each head of queries and keys and rotates it
  *   kv_cache_extend,       block tables and slot maps from request lengths, and
  *   kv_cache_release       pages back to the list of free ones
@@ -667,6 +667,29 @@ typedef struct {
 } tva_params;
 
 int32_t tree_verify_attention(smart_ctx* ctx, void* stream, const tva_params* params);
+
+/* ---------------------------------------------------------------------------
+ * tree_verify_attention_window (device)
+ *
+ * tree_verify_attention through a sliding window: a cached token's position is
+ * its index, a node whose anc_mask has k bits set (bits of its tree) is at
+ * position prefix_len + max(k - 1, 0), the j-th of these bits from the lowest
+ * up, from 0, at prefix_len + j (in a tree whose parents precede their children
+ * that is prefix_len + depth, tree_pack's position).  A node at position p sees
+ * those of its keys at positions x with p - x < window (itself among them) or
+ * x < sinks.  Nothing that another key holds enters its row.
+ * Of the block table only the entries of blocks that hold the first `sinks`
+ * tokens or tokens from prefix_len - window + 1 on are used, and checked
+ * (d_status): the others may have been given back (kv_cache_release).
+ * Every element type, layout, head_dim, block_size and cache of
+ * tree_verify_attention; softmax weights are held in fp32 (with a 4-bit cache, and
+ * where the window holds all that the table can, as there).  A captured call, and
+ * one for which there is no memory, takes the workspace-free form described at
+ * tree_verify_attention_static.
+ * Host errors: as tree_verify_attention, plus SMART_EINVAL for window < 1 or
+ * sinks < 0.
+ * ------------------------------------------------------------------------- */
+int32_t tree_verify_attention_window(smart_ctx* ctx, void* stream, const tva_params* params, int32_t window, int32_t sinks);
 
 /* ---------------------------------------------------------------------------
  * tree_verify_attention_static (device)

@@ -36,7 +36,8 @@ EXPORTS = ["smart_strerror", "smart_last_hip_error", "smart_create", "smart_dest
            "tree_upload_pack", "tree_pack",
            "kv_cache_write", "kv_cache_write_fp8", "tree_verify_attention", "tree_verify_attention_static", "tree_accept", "tree_accept_sample", "tree_commit", "tree_commit_fp8",
            "kv_cache_write_fp4", "kv_cache_read_fp4", "tree_commit_fp4", "prompt_attention",
-           "tree_norm_rope", "kv_cache_extend", "kv_cache_release", "prompt_attention_window"]
+           "tree_norm_rope", "kv_cache_extend", "kv_cache_release", "prompt_attention_window",
+           "tree_verify_attention_window"]
 
 
 class SmartError(RuntimeError):
@@ -192,6 +193,8 @@ def _lib():
                                         vp, vp, i64, i64, vp, vp]
         lib.prompt_attention.restype = i32
         lib.prompt_attention.argtypes = [vp, vp, ctypes.POINTER(PromptParams)]
+        lib.tree_verify_attention_window.restype = i32
+        lib.tree_verify_attention_window.argtypes = [vp, vp, ctypes.POINTER(TvaParams), i32, i32]
         lib.prompt_attention_window.restype = i32
         lib.prompt_attention_window.argtypes = [vp, vp, ctypes.POINTER(PromptParams), i32, i32]
         lib.tree_norm_rope.restype = i32
@@ -433,7 +436,8 @@ _NATIVE_ENTRIES = ("smart_select_begin_device", "smart_select_layer_device", "tr
                    "tree_rope", "kv_cache_write", "kv_cache_write_fp8", "tree_verify_attention",
                    "tree_verify_attention_static", "tree_accept", "tree_accept_sample", "tree_commit", "tree_commit_fp8",
                    "kv_cache_write_fp4", "kv_cache_read_fp4", "tree_commit_fp4", "prompt_attention",
-                   "tree_norm_rope", "kv_cache_extend", "kv_cache_release", "prompt_attention_window")
+                   "tree_norm_rope", "kv_cache_extend", "kv_cache_release", "prompt_attention_window",
+                   "tree_verify_attention_window")
 _nativeh = None
 
 
@@ -666,14 +670,15 @@ class SmartTree:
     def tree_verify_attention(self, q, k_tree, v_tree, k_cache, v_cache, block_table, prefix_len,
                               cu_nodes, anc_mask, softmax_scale, kv_layout, block_size=16,
                               out=None, lse=None, want_lse=False, h_cu_nodes=None, k_scale=None, v_scale=None,
-                              static=False, status=None, kv_cache_dtype=None):
+                              static=False, status=None, kv_cache_dtype=None, window=None, sinks=0):
         """k_cache / v_cache: [num_blocks, Hkv, ...] with one contiguous page of
         block_size * D elements per (block, head) (any of the two layouts).
         ``status``: optional int32 [B] tensor that receives the per-sequence block-table check.
         ``static``: call tree_verify_attention_static (no device allocation inside the library;
         pass ``out`` / ``lse`` so that nothing is allocated here either).
         ``kv_cache_dtype``: SMART_FP4_E2M1 for 4-bit caches (uint8 [num_blocks, Hkv, fp4_page_bytes(block_size, D)],
-        kv_layout SMART_KV_INTERLEAVED); otherwise the tensors' type tells (uint8: fp8)."""
+        kv_layout SMART_KV_INTERLEAVED); otherwise the tensors' type tells (uint8: fp8).
+        ``window``: a node sees the last ``window`` positions up to its own only, and the first ``sinks`` tokens."""
         h_address = 0
         if h_cu_nodes is not None:      # numpy int32 [B+1], host copy of cu_nodes
             h_cu_nodes = np.ascontiguousarray(h_cu_nodes, np.int32)
@@ -683,8 +688,16 @@ class SmartTree:
             raise ValueError(f"kv_cache_dtype {kv_cache_dtype!r}")
         if kv_cache_dtype == SMART_FP8_E4M3 and k_cache is not None and k_cache.dtype != _torch().uint8:
             raise ValueError(f"kv_cache_dtype SMART_FP8_E4M3, but the caches hold {k_cache.dtype}")
-        if kv_cache_dtype == SMART_FP4_E2M1:
+        if kv_cache_dtype == SMART_FP4_E2M1 or window is not None:
             self._here(q)
+        if window is not None:
+            if static:
+                raise ValueError("a call with a window has no static form (a captured one allocates nothing)")
+            return self._native.attention_window(self._ctx, q, k_tree, v_tree, k_cache, v_cache, block_table, prefix_len, cu_nodes,
+                                                 anc_mask, softmax_scale, kv_layout, block_size, out, lse, want_lse, h_address,
+                                                 k_scale, v_scale, False, status, window, sinks, kv_cache_dtype == SMART_FP4_E2M1)
+        if sinks:
+            raise ValueError("sinks without a window")
         call = self._native.attention_fp4 if kv_cache_dtype == SMART_FP4_E2M1 else self._native.attention
         return call(self._ctx, q, k_tree, v_tree, k_cache, v_cache, block_table, prefix_len, cu_nodes,
                     anc_mask, softmax_scale, kv_layout, block_size, out, lse, want_lse, h_address, k_scale, v_scale, static,

@@ -99,18 +99,24 @@ inline bool fp4_cache_ok(int64_t block_size, int64_t head_dim, const void* k_cac
 }
 // Argument checks of tree_verify_attention (host only; nothing is enqueued).
 int32_t tva_check_params(const tva_params& p);
-// Entry points of the attention implementations (validated params).  `fixed`: the buffers to use
+// A sliding window (at least 1) and the first tokens that stay visible.
+struct TvaWindow {
+  int32_t window, sinks;
+};
+// Entry points of the attention implementations (validated params; `window`: NULL for none).  `fixed`: the buffers to use
 // instead of the context's own growable workspace (then nothing is allocated; SMART_ECAP if they are too small).
-int32_t tva_launch_general(smart_ctx* ctx, hipStream_t stream, const tva_params& p);
+int32_t tva_launch_general(smart_ctx* ctx, hipStream_t stream, const tva_params& p, const TvaWindow* window = nullptr);
 int32_t tva_launch_mfma(smart_ctx* ctx, hipStream_t stream, const tva_params& p, const TvaWorkspace* fixed);
 // The tiled matrix-core path: every other type, layout, head dim and block size whose rows are aligned.
-int32_t tva_launch_tiled(smart_ctx* ctx, hipStream_t stream, const tva_params& p, const TvaWorkspace* fixed);
+int32_t tva_launch_tiled(smart_ctx* ctx, hipStream_t stream, const tva_params& p, const TvaWorkspace* fixed,
+                         const TvaWindow* window = nullptr);
 bool tva_tiled_supported(const tva_params& p);
 // Its buffer for any call of at most these sizes (head counts that divide in any way, any head dim).
 size_t tva_tiled_reserve(const smart_ctx* ctx, int32_t batch, int32_t total_nodes, int32_t num_q_heads,
                          int32_t num_kv_heads);
 // Dispatch between them (validated params, the context's device current).
-int32_t tva_dispatch(smart_ctx* ctx, hipStream_t stream, const tva_params& p, const TvaWorkspace* fixed);
+int32_t tva_dispatch(smart_ctx* ctx, hipStream_t stream, const tva_params& p, const TvaWorkspace* fixed,
+                     const TvaWindow* window = nullptr);
 // This device's copy of the library's static scratch array (the device must be current); resolved once per device.
 int32_t static_scratch(int device, void** ptr, size_t* bytes);
 bool tva_mfma_supported(const tva_params& p);
@@ -122,16 +128,27 @@ int32_t tva_mfma_default_workers(const smart_ctx* ctx);
 #ifdef __HIPCC__
 // One wavefront checks the block-table entries a call reads for sequence b (the first ceil(len / block_size) of its
 // row, len clamped like the kernels clamp it) and writes status[b]: 0, or SMART_TVA_BAD_BLOCK if one of them lies
-// outside [0, num_blocks) (the kernels read such an entry as the nearest valid block).
+// outside [0, num_blocks) (the kernels read such an entry as the nearest valid block).  With a window the call reads the entries
+// of the first `sinks` tokens and those from the block of token len - window + 1 on.
+template <bool kWindow = false>
 __device__ inline void tva_validate_block_table(int b, const int32_t* block_table, const int32_t* prefix_len,
                                                 int max_blocks, int block_size, int num_blocks, int32_t* status,
-                                                int lane) {
+                                                int lane, int window = 0, int sinks = 0) {
   const int cap = max_blocks * block_size;
   int len = prefix_len[b];
   len = len < 0 ? 0 : (len > cap ? cap : len);
   const int n_blocks = (len + block_size - 1) / block_size;
   bool bad = false;
-  for (int i = lane; i < n_blocks; i += 64) {
+  int first = 0;
+  if (kWindow) {
+    first = len >= window ? (len - window + 1) / block_size : 0;
+    const int until = min(first, (int)(((int64_t)sinks + block_size - 1) / block_size));
+    for (int i = lane; i < until; i += 64) {
+      const int32_t e = block_table[(size_t)b * max_blocks + i];
+      bad = bad || e < 0 || e >= num_blocks;
+    }
+  }
+  for (int i = first + lane; i < n_blocks; i += 64) {
     const int32_t e = block_table[(size_t)b * max_blocks + i];
     bad = bad || e < 0 || e >= num_blocks;
   }

@@ -38,6 +38,7 @@ struct Entries {
   decltype(&kv_cache_extend) cache_extend;
   decltype(&kv_cache_release) cache_release;
   decltype(&prompt_attention_window) prompt_window;
+  decltype(&tree_verify_attention_window) attention_window;
 } lib;
 PyObject *check_call, *get_device, *raw_stream;
 
@@ -651,13 +652,13 @@ void attention_tensors(PyObject* const* a) {
 }
 
 // ctx, q, k_tree, v_tree, k_cache, v_cache, block_table, prefix_len, cu_nodes, anc_mask, scale, layout, block_size, out, lse,
-// want_lse, address of the host's offsets, k_scale, v_scale, static, status
-template <bool kFp4>
+// want_lse, address of the host's offsets, k_scale, v_scale, static, status (, window, sinks, whether the cache holds 4 bits)
+template <bool kFp4, bool kWindow>
 PyObject* attention_over(PyObject* const* a) {
   auto ctx = pointer<smart_ctx>(a[0]);
   const at::Tensor &q = tensor(a[1]), &kt = tensor(a[2]), &vt = tensor(a[3]), &cu = tensor(a[8]);
   three_dims(q);
-  if (kFp4) attention_tensors(a);
+  if (kFp4 || kWindow) attention_tensors(a);
   at::Tensor out = a[13] == Py_None ? at::empty_like(q) : tensor(a[13]), lse;
   const bool want_lse = truth(a[15]);
   tva_params p = {};
@@ -693,6 +694,13 @@ PyObject* attention_over(PyObject* const* a) {
       p.cache_token_stride = kc.stride(2);
     }
     p.d_block_table = address<int32_t>(tensor(a[6]));
+    if (kWindow && !kFp4) {
+      const bool types = kc.scalar_type() == vc.scalar_type() && (kc.scalar_type() == at::kByte || kc.scalar_type() == q.scalar_type());
+      if (!types || kc.size(0) != vc.size(0) || kc.size(1) != p.num_kv_heads || vc.size(1) != p.num_kv_heads) {
+        PyErr_SetString(PyExc_ValueError, "tree_verify_attention: caches [num_blocks, num_kv_heads, ...] of the queries' element type or uint8");
+        throw Failed();
+      }
+    }
     if (kFp4) {
       page_bytes(kc, vc, p.num_kv_heads, p.block_size, p.head_dim);
       p.kv_cache_dtype = SMART_FP4_E2M1;
@@ -714,14 +722,18 @@ PyObject* attention_over(PyObject* const* a) {
   p.d_lse = lse.defined() ? address<float>(lse) : nullptr;
   p.d_status = address<int32_t>(a[20]);
   p.h_cu_nodes = pointer<const int32_t>(a[16]);
-  void* s = kFp4 ? stream(&q) : stream();
-  if (truth(a[19])) call("tree_verify_attention_static", [&] { return lib.attention_static(ctx, s, &p); });
+  void* s = kFp4 || kWindow ? stream(&q) : stream();
+  if (kWindow) {
+    const int32_t window = integer32(a[21]), sinks = integer32(a[22]);
+    call("tree_verify_attention_window", [&] { return lib.attention_window(ctx, s, &p, window, sinks); });
+  } else if (truth(a[19])) call("tree_verify_attention_static", [&] { return lib.attention_static(ctx, s, &p); });
   else call("tree_verify_attention", [&] { return lib.attention(ctx, s, &p); });
   return lse.defined() ? tuple_of(out, lse) : wrap(out);
 }
 
-PyObject* attention(PyObject* const* a) { return attention_over<false>(a); }
-PyObject* attention_fp4(PyObject* const* a) { return attention_over<true>(a); }
+PyObject* attention(PyObject* const* a) { return attention_over<false, false>(a); }
+PyObject* attention_fp4(PyObject* const* a) { return attention_over<true, false>(a); }
+PyObject* attention_window(PyObject* const* a) { return truth(a[23]) ? attention_over<true, true>(a) : attention_over<false, true>(a); }
 
 PyObject* accept(PyObject* const* a) {  // ctx, cu_nodes, parent, token, target_next, max_depth
   auto ctx = pointer<smart_ctx>(a[0]);
@@ -798,7 +810,7 @@ PyMethodDef methods[] = {SMART_METHOD(setup, 4),       SMART_METHOD(select_begin
                          SMART_METHOD(attention_fp4, 21), SMART_METHOD(cache_write_fp4, 7), SMART_METHOD(cache_read_fp4, 7),
                          SMART_METHOD(commit_fp4, 11), SMART_METHOD(prompt, 9),
                          SMART_METHOD(norm_rope, 12), SMART_METHOD(cache_extend, 10), SMART_METHOD(cache_release, 11),
-                         SMART_METHOD(prompt_window, 11),
+                         SMART_METHOD(prompt_window, 11), SMART_METHOD(attention_window, 24),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef marshal_module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

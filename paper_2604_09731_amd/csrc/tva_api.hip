@@ -45,8 +45,14 @@ int32_t tva_check_params(const tva_params& p) {
   return SMART_OK;
 }
 
-int32_t tva_dispatch(smart_ctx* ctx, hipStream_t stream, const tva_params& p, const TvaWorkspace* fixed) {
+int32_t tva_dispatch(smart_ctx* ctx, hipStream_t stream, const tva_params& p, const TvaWorkspace* fixed, const TvaWindow* window) {
   if (p.batch == 0 || p.total_nodes == 0) return SMART_OK;
+  // (a window that holds the longest prefix and the deepest tree hides nothing)
+  if (window && window->window >= (int64_t)p.max_blocks_per_seq * p.block_size + SMART_MAX_NODES) window = nullptr;
+  if (window) {
+    if (!ctx->opt_force_general && tva_tiled_supported(p)) return tva_launch_tiled(ctx, stream, p, fixed, window);
+    return tva_launch_general(ctx, stream, p, window);
+  }
   if (!ctx->opt_force_general && p.max_blocks_per_seq > 0 && tva_mfma_supported(p))
     return tva_launch_mfma(ctx, stream, p, fixed);
   if (!ctx->opt_force_general && tva_tiled_supported(p)) return tva_launch_tiled(ctx, stream, p, fixed);
@@ -55,14 +61,24 @@ int32_t tva_dispatch(smart_ctx* ctx, hipStream_t stream, const tva_params& p, co
 
 }  // namespace smart
 
-extern "C" int32_t tree_verify_attention(smart_ctx* ctx, void* stream, const tva_params* params) {
-  if (!ctx || !params) return SMART_EINVAL;
-  int32_t rc = smart::tva_check_params(*params);
+static int32_t attention(smart_ctx* ctx, void* stream, const tva_params& p, const smart::TvaWindow* window) {
+  int32_t rc = smart::tva_check_params(p);
   if (rc != SMART_OK) return rc;
   int prev = 0;
   SMART_HIP_CHECK(hipGetDevice(&prev));
   if (prev != ctx->device) SMART_HIP_CHECK(hipSetDevice(ctx->device));
-  rc = smart::tva_dispatch(ctx, (hipStream_t)stream, *params, nullptr);
+  rc = smart::tva_dispatch(ctx, (hipStream_t)stream, p, nullptr, window);
   if (prev != ctx->device) (void)hipSetDevice(prev);
   return rc;
+}
+
+extern "C" int32_t tree_verify_attention(smart_ctx* ctx, void* stream, const tva_params* params) {
+  if (!ctx || !params) return SMART_EINVAL;
+  return attention(ctx, stream, *params, nullptr);
+}
+
+extern "C" int32_t tree_verify_attention_window(smart_ctx* ctx, void* stream, const tva_params* params, int32_t window, int32_t sinks) {
+  if (!ctx || !params || window < 1 || sinks < 0) return SMART_EINVAL;
+  const smart::TvaWindow w{window, sinks};
+  return attention(ctx, stream, *params, &w);
 }

@@ -7,7 +7,8 @@
 // Per (node i, head h): keys are the sequence's cached prefix followed by the
 // tree nodes in anc_mask[i]; out = softmax(scale * q.k) . v over those keys
 // (the attention sub-step of verifying a draft tree in one target forward
-// pass, Sec. 1 of the paper).
+// pass, Sec. 1 of the paper).  With a window, those of them that a node sees
+// through it, and the first tokens.
 #include <math.h>
 
 #include "common.h"
@@ -74,10 +75,10 @@ __device__ inline float cached_v(const Fp4* cache, const Layout& lay, int64_t bl
 
 // T: element type of q, tree k / v and out; C: element type of the cache (T, uint8_t = E4M3 whose values are multiplied by
 // k_scale / v_scale, or Fp4).
-template <typename T, typename C>
+template <typename T, typename C, bool kWindow>
 __global__ __launch_bounds__(kWave) void tva_general_kernel(
     int batch, int total_nodes, int Hq, int Hkv, int D, int max_blocks, int num_blocks, float scale,
-    float k_scale, float v_scale,
+    float k_scale, float v_scale, int window, int sinks,
     Layout lay, const T* __restrict__ q, const T* __restrict__ k_tree, const T* __restrict__ v_tree,
     const C* __restrict__ k_cache, const C* __restrict__ v_cache,
     const int32_t* __restrict__ block_table, const int32_t* __restrict__ prefix_len,
@@ -89,7 +90,8 @@ __global__ __launch_bounds__(kWave) void tva_general_kernel(
   // block-table check: the wavefronts share the sequences between them
   if (status)
     for (int b = row; b < batch; b += gridDim.x)
-      smart::tva_validate_block_table(b, block_table, prefix_len, max_blocks, lay.block_size, num_blocks, status, lane);
+      smart::tva_validate_block_table<kWindow>(b, block_table, prefix_len, max_blocks, lay.block_size, num_blocks, status, lane, window,
+                                               sinks);
   const int node = row / Hq, h = row % Hq;
   if (node >= total_nodes) return;
   const int g = h / (Hq / Hkv);
@@ -114,7 +116,15 @@ __global__ __launch_bounds__(kWave) void tva_general_kernel(
     if (lse && lane == 0) lse[(size_t)node * Hq + h] = -INFINITY;
     return;
   }
-  const uint64_t mask_lo = anc_mask[2 * (size_t)node], mask_hi = anc_mask[2 * (size_t)node + 1];
+  uint64_t mask_lo = anc_mask[2 * (size_t)node], mask_hi = anc_mask[2 * (size_t)node + 1];
+  int set = 0, begin = 0;  // nodes of the mask, and the first token behind the first ones that the window holds
+  if (kWindow) {
+    if (n_b < 64) mask_lo &= (1ull << n_b) - 1ull, mask_hi = 0ull;
+    else if (n_b < 128) mask_hi &= (1ull << (n_b - 64)) - 1ull;
+    set = (int)__popcll((unsigned long long)mask_lo) + (int)__popcll((unsigned long long)mask_hi);
+    const int64_t first = (int64_t)len + (set > 0 ? set - 1 : 0) - window + 1;
+    begin = (int)(first < 0 ? 0 : (first > len ? len : first));
+  }
 
   for (int d = lane; d < D; d += kWave) s_q[d] = to_float(q[((size_t)node * Hq + h) * D + d]);
   __syncthreads();
@@ -124,19 +134,25 @@ __global__ __launch_bounds__(kWave) void tva_general_kernel(
   const int n_tree_chunks = (n_b + kWave - 1) / kWave;
 
   for (int c = 0; c < n_prefix_chunks + n_tree_chunks; ++c) {
+    if (kWindow && c < begin / kWave && c * kWave >= sinks) c = begin / kWave;  // over the gap
     const bool tree = c >= n_prefix_chunks;
     const int idx = (tree ? (c - n_prefix_chunks) : c) * kWave + lane;  // token or local node
     bool valid;
     int slot = 0;
     int64_t blk = 0;
     if (!tree) {
-      valid = idx < len;
+      valid = idx < len && !(kWindow && idx >= sinks && idx < begin);
       const int t = valid ? idx : 0;
       blk = block_table[(size_t)b * max_blocks + t / lay.block_size];
       blk = blk < 0 ? 0 : (blk >= num_blocks ? num_blocks - 1 : blk);
       slot = t % lay.block_size;
     } else {
       valid = idx < n_b && ((idx < 64 ? (mask_lo >> idx) : (mask_hi >> (idx - 64))) & 1ull);
+      if (kWindow && valid) {  // the k-th node of the mask is at position len + k, this row at that of the last
+        const uint64_t low = idx < 64 ? mask_lo & ((1ull << idx) - 1ull) : mask_lo, high = idx < 64 ? 0ull : mask_hi & ((1ull << (idx - 64)) - 1ull);
+        const int k = (int)__popcll((unsigned long long)low) + (int)__popcll((unsigned long long)high);
+        valid = set - 1 - k < window || k < sinks - len;
+      }
     }
     const int j = valid ? idx : 0;
     float s = -INFINITY;
@@ -191,7 +207,7 @@ __global__ __launch_bounds__(kWave) void tva_general_kernel(
 
 namespace smart {
 
-int32_t tva_launch_general(smart_ctx* ctx, hipStream_t stream, const tva_params& p) {
+int32_t tva_launch_general(smart_ctx* ctx, hipStream_t stream, const tva_params& p, const TvaWindow* window) {
   const int64_t rows = (int64_t)p.total_nodes * p.num_q_heads;
   if (rows == 0) return SMART_OK;
   if (rows > 0x7FFFFFFF) return SMART_EINVAL;
@@ -201,17 +217,21 @@ int32_t tva_launch_general(smart_ctx* ctx, hipStream_t stream, const tva_params&
   if (rc != SMART_OK) return rc;
   const bool fp8 = p.kv_cache_dtype == SMART_FP8_E4M3, fp4 = p.kv_cache_dtype == SMART_FP4_E2M1;
   const float ks = fp8 ? p.k_scale : 1.f, vs = fp8 ? p.v_scale : 1.f;
+  const TvaWindow w = window ? *window : TvaWindow{0, 0};
 #define SMART_LAUNCH_GENERAL(T, C)                                                                            \
-  hipLaunchKernelGGL((tva_general_kernel<T, C>), dim3((unsigned)rows), dim3(kWave), 0, stream, p.batch,      \
+  if (window) SMART_LAUNCH_KIND(T, C, true); else SMART_LAUNCH_KIND(T, C, false)
+#define SMART_LAUNCH_KIND(T, C, WINDOW)                                                                       \
+  hipLaunchKernelGGL((tva_general_kernel<T, C, WINDOW>), dim3((unsigned)rows), dim3(kWave), 0, stream, p.batch,      \
                      p.total_nodes, p.num_q_heads, p.num_kv_heads, p.head_dim, p.max_blocks_per_seq,         \
-                     p.num_blocks, p.softmax_scale, ks, vs, lay, (const T*)p.d_q, (const T*)p.d_k_tree,      \
+                     p.num_blocks, p.softmax_scale, ks, vs, w.window, w.sinks, lay, (const T*)p.d_q, (const T*)p.d_k_tree, \
                      (const T*)p.d_v_tree, (const C*)p.d_k_cache, (const C*)p.d_v_cache, p.d_block_table,    \
                      p.d_prefix_len, p.d_cu_nodes, p.d_anc_mask, (T*)p.d_out, p.d_lse, p.d_status)
   if (p.dtype == SMART_F32) {
-    if (fp4) SMART_LAUNCH_GENERAL(float, Fp4); else if (fp8) SMART_LAUNCH_GENERAL(float, uint8_t); else SMART_LAUNCH_GENERAL(float, float);
+    if (fp4) { SMART_LAUNCH_GENERAL(float, Fp4); } else if (fp8) { SMART_LAUNCH_GENERAL(float, uint8_t); } else { SMART_LAUNCH_GENERAL(float, float); }
   } else {
-    if (fp4) SMART_LAUNCH_GENERAL(uint16_t, Fp4); else if (fp8) SMART_LAUNCH_GENERAL(uint16_t, uint8_t); else SMART_LAUNCH_GENERAL(uint16_t, uint16_t);
+    if (fp4) { SMART_LAUNCH_GENERAL(uint16_t, Fp4); } else if (fp8) { SMART_LAUNCH_GENERAL(uint16_t, uint8_t); } else { SMART_LAUNCH_GENERAL(uint16_t, uint16_t); }
   }
+#undef SMART_LAUNCH_KIND
 #undef SMART_LAUNCH_GENERAL
   SMART_HIP_CHECK(hipGetLastError());
   return profile_end(ctx, stream);

@@ -47,6 +47,8 @@
 // The paper (Sec. 1) has the target model verify the tree in one forward pass; this is the attention sub-step.
 #include <math.h>
 
+#include <algorithm>
+
 #include "common.h"
 #include "fp4.h"
 #include "wave.h"
@@ -108,6 +110,7 @@ struct TiledArgs {
   int64_t block_stride, head_stride, token_stride;
   int32_t batch, total_nodes, Hq, Hkv, G, block_size, max_blocks, num_blocks;
   int32_t segment_cost, tree_cost;  // units of a segment beside its steps, and of 32 nodes of its tree
+  int32_t window, sinks;  // of a call with a window
   bool fp8, fp4, plain;   // the cache's element type and layout, where they are no template arguments
   bool stream;            // the prefix kernel streams, and evaluates the trees of sequences with a prefix
   bool spread;            // direct form: consecutive segments go to different L2s
@@ -128,19 +131,38 @@ template <typename T> struct StepCost;
 template <> struct StepCost<__bf16> { static constexpr int one = 4, two = 5, four = 8; };
 template <> struct StepCost<float> { static constexpr int one = 4, two = 7, four = 14; };
 
+// A prefix seen through a window: what some node sees of it, the first `sinks` tokens and those that the root's window holds, as
+// keys without the gap between them.  Key v is token v, or v + shift from `gap` on.  Gap and shift are multiples of 8: groups of eight
+// keys are groups of eight tokens, in one page.  No other page is read (the page of the first key holds a token that is seen).
+template <bool kWindow>
+struct Span {
+  int shift = 0, gap = 0;
+  __device__ int token(int v) const { return kWindow && v >= gap ? v + shift : v; }
+};
+template <bool kWindow>
+__device__ inline Span<kWindow> span_of(const TiledArgs& a, int len) {
+  Span<kWindow> s;
+  if (kWindow) {
+    const int first = (int)max((int64_t)0, (int64_t)len - a.window + 1) & ~7, until = (int)min(((int64_t)a.sinks + 7) & ~(int64_t)7, (int64_t)0x7FFFFFF8);
+    if (first > until) s.shift = first - until, s.gap = until;
+  }
+  return s;
+}
+
 // What a call uses of one sequence: lengths and sizes clamped to what the arrays hold.  A range that leaves the arrays
 // has no rows (nothing of it is read).
 struct Shape {
-  int len, base, n, rows, groups, steps;
+  int len, base, n, rows, groups, steps;  // len: keys (with a window fewer than the prefix has tokens)
   int cost_last, extra;  // units of a step of the last row group (the others: StepCost::four), of a segment beside its steps
   int64_t full, head;  // units of a full row group, of a kv head
 };
 
-template <typename T>
+template <typename T, bool kWindow>
 __device__ inline Shape shape_of(const TiledArgs& a, int len, int base, int next) {
   Shape s;
   const int cap = a.max_blocks * a.block_size;
   s.len = len < 0 ? 0 : (len > cap ? cap : len);
+  if (kWindow) s.len -= span_of<kWindow>(a, s.len).shift;
   int64_t n = (int64_t)next - base;
   n = n < 0 ? 0 : (n > SMART_MAX_NODES ? SMART_MAX_NODES : n);
   if (base < 0 || base + n > a.total_nodes) n = 0;
@@ -175,12 +197,12 @@ constexpr int kIrregular = 2;   // a range leaves the arrays or holds more nodes
 
 // One wavefront goes through chunks c0 .. c1 - 1 of 64 sequences: visit(first sequence, lane has one, its units and segments,
 // units and segments before it); `sums` moves from before the chunks to behind them.
-template <typename T, typename Visit>
+template <typename T, bool kWindow, typename Visit>
 __device__ inline void scan_batch(const TiledArgs& a, int lane, int c0, int c1, Sums* sums, Visit visit) {
   for (int b0 = c0 * kWave; b0 < min(c1 * kWave, a.batch); b0 += kWave) {
     const int b = min(b0 + lane, a.batch - 1);
     const int base = a.cu_nodes[b], next = a.cu_nodes[b + 1];
-    const Shape s = shape_of<T>(a, a.prefix_len[b], base, next);
+    const Shape s = shape_of<T, kWindow>(a, a.prefix_len[b], base, next);
     const bool there = b0 + lane < a.batch;
     if (__any(next < base)) sums->flags |= kDescending;
     if (__any(s.n != (int64_t)next - base)) sums->flags |= kIrregular;
@@ -195,6 +217,21 @@ __device__ inline void scan_batch(const TiledArgs& a, int lane, int c0, int c1, 
     sums->segs += ts;
     sums->steps += tt;
   }
+}
+
+// The prefix's length, clamped to what the table holds.
+__device__ inline int length_of(const TiledArgs& a, int b) {
+  const int len = a.prefix_len[b], cap = a.max_blocks * a.block_size;
+  return len < 0 ? 0 : (len > cap ? cap : len);
+}
+// The first key behind the first tokens that a node sees through its window, which may be behind the last key: a node whose mask
+// has k bits set (within its tree of n) is at position len + max(k - 1, 0).
+__device__ inline int window_begin(const TiledArgs& a, const Span<true>& span, int len, int node, int n) {
+  uint64_t lo = a.anc_mask[2 * (size_t)node], hi = a.anc_mask[2 * (size_t)node + 1];
+  if (n < 64) lo &= (1ull << n) - 1ull, hi = 0ull;
+  else if (n < 128) hi &= (1ull << (n - 64)) - 1ull;
+  const int set = (int)__popcll((unsigned long long)lo) + (int)__popcll((unsigned long long)hi), depth = set > 0 ? set - 1 : 0;
+  return (int)min((int64_t)len, max((int64_t)0, (int64_t)len + depth - a.window + 1)) - span.shift;
 }
 
 __device__ inline int clamp_block(int b, int num_blocks) { return b < 0 ? 0 : (b >= num_blocks ? num_blocks - 1 : b); }
@@ -315,29 +352,33 @@ struct Stager {
   }
   // Token of a key of the step, kept inside the prefix (what lies past it is masked later): a V vector of an
   // interleaved page starts at a multiple of 8.
-  __device__ static int token_k(int step, int key, int len) { return min(step * kStepKeys + key, len - 1); }
-  __device__ static int token_v(int step, int key, int len) {
-    return kPlain ? token_k(step, key, len) : min(step * kStepKeys + key, (len - 1) & ~7);
+  template <bool kWindow>
+  __device__ static int token_k(const Span<kWindow>& span, int step, int key, int len) { return span.token(min(step * kStepKeys + key, len - 1)); }
+  template <bool kWindow>
+  __device__ static int token_v(const Span<kWindow>& span, int step, int key, int len) {
+    return kPlain ? token_k(span, step, key, len) : span.token(min(step * kStepKeys + key, (len - 1) & ~7));
   }
   __device__ static int block_of(const TiledArgs& a, int token) {
     return (int)__umulhi(((uint32_t)token >> 3) << 1, a.block8_magic);
   }
 
-  __device__ void load_ids(const TiledArgs& a, const int32_t* row, int step, int len, int tid) {
+  template <bool kWindow>
+  __device__ void load_ids(const TiledArgs& a, const Span<kWindow>& span, const int32_t* row, int step, int len, int tid) {
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
-      idk[i] = row[block_of(a, token_k(step, key_of_k(i * kThreads + tid), len))];
-      if (!kPlain) idv[i] = row[block_of(a, token_v(step, key_of_v(i * kThreads + tid), len))];
+      idk[i] = row[block_of(a, token_k(span, step, key_of_k(i * kThreads + tid), len))];
+      if (!kPlain) idv[i] = row[block_of(a, token_v(span, step, key_of_v(i * kThreads + tid), len))];
     }
   }
-  __device__ void load(const TiledArgs& a, int step, int len, int g, int tid) {
+  template <bool kWindow>
+  __device__ void load(const TiledArgs& a, const Span<kWindow>& span, int step, int len, int g, int tid) {
     constexpr int kB = kFp8 ? 1 : (int)sizeof(T);  // bytes of a cache element
     const char* kc = (const char*)a.k_cache + (int64_t)g * a.head_stride * kB;
     const char* vc = (const char*)a.v_cache + (int64_t)g * a.head_stride * kB;
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
       const int p = i * kThreads + tid;
-      const int tk = token_k(step, key_of_k(p), len);
+      const int tk = token_k(span, step, key_of_k(p), len);
       const int64_t at = clamp_block(idk[i], a.num_blocks) * a.block_stride +
                          offset_k(a, p, tk - block_of(a, tk) * a.block_size);
       k[i] = *(const Raw*)(kc + at * kB);
@@ -347,7 +388,7 @@ struct Stager {
 #pragma unroll
       for (int i = 0; i < kPer; ++i) {
         const int p = i * kThreads + tid;
-        const int tv = token_v(step, key_of_v(p), len);
+        const int tv = token_v(span, step, key_of_v(p), len);
         const int64_t at = clamp_block(idv[i], a.num_blocks) * a.block_stride +
                            offset_v(a, p, tv - block_of(a, tv) * a.block_size);
         v[i] = *(const Raw*)(vc + at * kB);
@@ -445,17 +486,23 @@ struct Stager<T, kE2M1, false, D> {
   __device__ static int block_of(const TiledArgs& a, int token) {
     return (int)__umulhi(((uint32_t)token >> 3) << 1, a.block8_magic);
   }
-  __device__ static int token_k(int step, int p, int len) { return min(step * kStepKeys + key_of_k(p), len - 1); }
-  __device__ static int token_v(int step, int p, int len) { return min(step * kStepKeys + key_of_v(p), (len - 1) & ~7); }
-
-  __device__ void load_ids(const TiledArgs& a, const int32_t* row, int step, int len, int tid) {
-    if (kVectors < kThreads && tid >= kVectors) return;
-    idk = row[block_of(a, token_k(step, tid, len))];
-    idv = row[block_of(a, token_v(step, tid, len))];
+  template <bool kWindow>
+  __device__ static int token_k(const Span<kWindow>& span, int step, int p, int len) { return span.token(min(step * kStepKeys + key_of_k(p), len - 1)); }
+  template <bool kWindow>
+  __device__ static int token_v(const Span<kWindow>& span, int step, int p, int len) {
+    return span.token(min(step * kStepKeys + key_of_v(p), (len - 1) & ~7));
   }
-  __device__ void load(const TiledArgs& a, int step, int len, int g, int tid) {
+
+  template <bool kWindow>
+  __device__ void load_ids(const TiledArgs& a, const Span<kWindow>& span, const int32_t* row, int step, int len, int tid) {
     if (kVectors < kThreads && tid >= kVectors) return;
-    const int bs = a.block_size, tk = token_k(step, tid, len), tv = token_v(step, tid, len);
+    idk = row[block_of(a, token_k(span, step, tid, len))];
+    idv = row[block_of(a, token_v(span, step, tid, len))];
+  }
+  template <bool kWindow>
+  __device__ void load(const TiledArgs& a, const Span<kWindow>& span, int step, int len, int g, int tid) {
+    if (kVectors < kThreads && tid >= kVectors) return;
+    const int bs = a.block_size, tk = token_k(span, step, tid, len), tv = token_v(span, step, tid, len);
     const int sk = tk - block_of(a, tk) * bs, sv = tv - block_of(a, tv) * bs;
     const uint8_t* kp = (const uint8_t*)a.k_cache + clamp_block(idk, a.num_blocks) * a.block_stride + g * a.head_stride;
     const uint8_t* vp = (const uint8_t*)a.v_cache + clamp_block(idv, a.num_blocks) * a.block_stride + g * a.head_stride;
@@ -528,14 +575,17 @@ struct Rows<__bf16, kPlain, D> {
   floatx16 o[D / 32];
   float m, l;   // of row lane % 32; l: this half-wavefront's keys
   float exact;  // l of unrounded weights
+  int begins;   // with a window: the row's first key behind the first tokens
 
-  __device__ void begin(const TiledArgs& a, int base, int g, int row0, int rows, int lane) {
+  template <bool kWindow>
+  __device__ void begin(const TiledArgs& a, const Span<kWindow>& span, int len, int base, int n, int g, int row0, int rows, int lane) {
     const int h = lane >> 5, j = lane & 31;
     const int rho = min(row0 + j, rows - 1);  // padding rows repeat the last real row; never read back
     const int node = base + rho / a.G, head = g * a.G + rho % a.G;
     const __bf16* qp = (const __bf16*)a.q + ((int64_t)node * a.Hq + head) * D + h * 8;
 #pragma unroll
     for (int ks = 0; ks < D / 16; ++ks) q[ks] = *(const bf16x8*)(qp + ks * 16);
+    if constexpr (kWindow) begins = window_begin(a, span, len, node, n);
     reset();
   }
   __device__ void reset() {
@@ -546,8 +596,9 @@ struct Rows<__bf16, kPlain, D> {
   }
   __device__ static int key_of_row(int i) { return kPlain ? i : (i & 16) + sigma(i & 15); }
 
-  template <bool kInPlace, bool kOnePart, bool kExact>
-  __device__ void tile(const uintx4* kt, const uintx4* vt, int n_valid, float c, int lane) {
+  // key0: the tile's first key, of which those from `sinks` on are seen from `begins` on
+  template <bool kInPlace, bool kOnePart, bool kExact, bool kWindow>
+  __device__ void tile(const uintx4* kt, const uintx4* vt, int n_valid, int key0, int sinks, float c, int lane) {
     const int h = lane >> 5, j = lane & 31;
     const int key = key_of_row(j);
     bf16x8 kx[D / 16];  // all operands of a product are requested before its first MFMA
@@ -568,6 +619,13 @@ struct Rows<__bf16, kPlain, D> {
 #pragma unroll
       for (int r = 0; r < 16; ++r)
         if (key_of_row(8 * (r >> 2) + 4 * h + (r & 3)) >= n_valid) s[r] = -INFINITY;
+    }
+    if (kWindow && key0 + 32 > sinks && __any(key0 < begins)) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int at = key_of_row(8 * (r >> 2) + 4 * h + (r & 3));
+        if (at >= sinks - key0 && at < begins - key0) s[r] = -INFINITY;
+      }
     }
     float mx = s[0];
 #pragma unroll
@@ -652,8 +710,10 @@ struct Rows<float, kPlain, D> {
   floatx4 q[2][D / 16];
   floatx4 o[2][D / 16];
   float m[2], l[2];  // of rows lane % 16 and lane % 16 + 16; l: this quarter-wavefront's keys
+  int begins[2];     // with a window: the rows' first keys behind the first tokens
 
-  __device__ void begin(const TiledArgs& a, int base, int g, int row0, int rows, int lane) {
+  template <bool kWindow>
+  __device__ void begin(const TiledArgs& a, const Span<kWindow>& span, int len, int base, int n, int g, int row0, int rows, int lane) {
     const int quarter = lane >> 4, j = lane & 15;
 #pragma unroll
     for (int nh = 0; nh < 2; ++nh) {
@@ -662,6 +722,7 @@ struct Rows<float, kPlain, D> {
       const float* qp = (const float*)a.q + ((int64_t)node * a.Hq + head) * D + 4 * quarter;
 #pragma unroll
       for (int s = 0; s < D / 16; ++s) q[nh][s] = *(const floatx4*)(qp + 16 * s);
+      if constexpr (kWindow) begins[nh] = window_begin(a, span, len, node, n);
     }
     reset();
   }
@@ -674,8 +735,8 @@ struct Rows<float, kPlain, D> {
       l[nh] = 0.f;
     }
   }
-  template <bool kInPlace, bool kOnePart, bool kExact>
-  __device__ void tile(const uintx4* kt, const uintx4* vt, int n_valid, float c, int lane) {
+  template <bool kInPlace, bool kOnePart, bool kExact, bool kWindow>
+  __device__ void tile(const uintx4* kt, const uintx4* vt, int n_valid, int key0, int sinks, float c, int lane) {
     const int quarter = lane >> 4, i = lane & 15;
     floatx4 s[2] = {(floatx4)(0.f), (floatx4)(0.f)};
     // contraction step (t, e): the four quarters hold head dims 16 t + 4 quarter + e
@@ -691,6 +752,13 @@ struct Rows<float, kPlain, D> {
     }
     // register r of a lane: key 4 quarter + r
     const bool ragged = n_valid < 16;
+    if (kWindow && key0 + 16 > sinks && __any(key0 < max(begins[0], begins[1]))) {
+#pragma unroll
+      for (int nh = 0; nh < 2; ++nh)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (4 * quarter + r >= sinks - key0 && 4 * quarter + r < begins[nh] - key0) s[nh][r] = -INFINITY;
+    }
     floatx4 p[2];
     float m_new[2];
     bool move = false;
@@ -1154,7 +1222,7 @@ __device__ inline int owner_of(const TiledArgs& a, int node) {
 // what does not depend on each other is requested together: the mask and the query while the plan is looked up, the
 // next two tree keys while the last two are used, two partials at a time.  All lanes of a wavefront go through this
 // together (rows that are not `active` have no keys and are not written).
-template <typename T, int D, bool kExact>
+template <typename T, int D, bool kExact, bool kWindow>
 struct Finish {
   static constexpr int K4 = D / 32;
   typedef typename Four<T>::type Raw;
@@ -1197,10 +1265,28 @@ struct Finish {
     }
     return x;
   }
-  // The tree part: the set bits of the row's ancestor mask, lowest first, of a tree of n nodes.
-  __device__ void tree(const TiledArgs& a, int g, int base, int n, int e) {
-    if (n < 64) mlo &= (1ull << n) - 1ull, mhi = 0ull;  // never index past the tree
+  // What the row sees of a tree of n nodes over b's prefix: never past the tree, and with a window (the k-th set bit, from 0, is at
+  // position len + k, the row at that of the last) the last ones and those among the first tokens.
+  __device__ void limit(const TiledArgs& a, int n, int b) {
+    if (n < 64) mlo &= (1ull << n) - 1ull, mhi = 0ull;
     else if (n < 128) mhi &= (1ull << (n - 64)) - 1ull;
+    if (kWindow) {
+      const int left = (int)__popcll((unsigned long long)mlo) + (int)__popcll((unsigned long long)mhi) - a.window;  // nodes behind the window
+      if (left > 0) {
+        const int kept = max(a.sinks - length_of(a, b), 0);
+        uint64_t lo = mlo, hi = mhi;
+        for (int k = 0; k < left; ++k) {
+          const uint64_t bit_lo = lo & (0ull - lo), bit_hi = lo ? 0ull : hi & (0ull - hi);
+          lo &= ~bit_lo;
+          hi &= ~bit_hi;
+          if (k >= kept) mlo &= ~bit_lo, mhi &= ~bit_hi;
+        }
+      }
+    }
+  }
+  // The tree part: the set bits of the row's ancestor mask, lowest first, of a tree of n nodes of sequence b.
+  __device__ void tree(const TiledArgs& a, int g, int base, int n, int b, int e) {
+    limit(a, n, b);
     const T* kt = (const T*)a.k_tree + ((int64_t)base * a.Hkv + g) * D;
     const T* vt = (const T*)a.v_tree + ((int64_t)base * a.Hkv + g) * D;
     const int64_t node_stride = (int64_t)a.Hkv * D;
@@ -1277,16 +1363,23 @@ struct Finish {
     asm volatile("" : "+v"(row));  // everything is derived anew, so that nothing lives in registers until here
     const int node = (int)(row / a.Hq), head = (int)(row % a.Hq), g = head / a.G;
     const int b = owner_of(a, node);
-    const Shape sh = shape_of<T>(a, a.prefix_len[b], a.cu_nodes[b], a.cu_nodes[b + 1]);
+    const Shape sh = shape_of<T, kWindow>(a, a.prefix_len[b], a.cu_nodes[b], a.cu_nodes[b + 1]);
     Finish f;
     f.request(a, node, head, active, e);
-    const int len = active ? sh.len : 0;
+    const int len = active ? sh.len : 0;  // keys
+    Span<kWindow> span;
+    int begins = 0;
+    if constexpr (kWindow) {
+      const int tokens = length_of(a, b);
+      span = span_of<kWindow>(a, tokens);
+      begins = window_begin(a, span, tokens, node, sh.n);
+    }
     constexpr int kAtOnce = 2;  // keys whose loads are in flight together (the last one again past the end)
     for (int t0 = 0; __any(t0 < len); t0 += kAtOnce) {
       floatx4 k4[kAtOnce][K4], v4[kAtOnce][K4];
 #pragma unroll
       for (int u = 0; u < kAtOnce; ++u) {
-        const int t = max(0, min(t0 + u, len - 1)), block = t / a.block_size, slot = t - block * a.block_size;
+        const int t = span.token(max(0, min(t0 + u, len - 1))), block = t / a.block_size, slot = t - block * a.block_size;
         const int64_t page = clamp_block(a.block_table[(int64_t)b * a.max_blocks + block], a.num_blocks) * a.block_stride +
                              g * a.head_stride;
 #pragma unroll
@@ -1302,8 +1395,12 @@ struct Finish {
         }
       }
 #pragma unroll
-      for (int u = 0; u < kAtOnce; ++u) f.add_key(k4[u], v4[u], t0 + u < len, a.m_scale, a.o_scale, a.c);
+      for (int u = 0; u < kAtOnce; ++u) {
+        const bool seen = t0 + u < len && !(kWindow && t0 + u >= a.sinks && t0 + u < begins);
+        f.add_key(k4[u], v4[u], seen, a.m_scale, a.o_scale, a.c);
+      }
     }
+    f.limit(a, sh.n, b);
     const T* kt = (const T*)a.k_tree + ((int64_t)sh.base * a.Hkv + g) * D;
     const T* vt = (const T*)a.v_tree + ((int64_t)sh.base * a.Hkv + g) * D;
     for (int j = 0; __any(active && j < sh.n); ++j) {
@@ -1379,11 +1476,11 @@ __device__ inline void zero_row(const TiledArgs& a, int64_t row, int e) {
 }
 
 // ---- the prefix kernel ----------------------------------------------------------------------------------------------------
-template <typename T, CacheType kCache, bool kPlain, int D, bool kDirect, bool kExact>
+template <typename T, CacheType kCache, bool kPlain, int D, bool kDirect, bool kExact, bool kWindow>
 __global__ __launch_bounds__(kThreads, 2) void tva_tiled_kernel(TiledArgs a) {
   typedef Stager<T, kCache, kPlain, D> Stage;
   typedef Fp4Stream<kExact> Stream;
-  constexpr bool kStream = streams<T>(kCache, D), kRounded = rounds_weights<T>(kCache);
+  constexpr bool kStream = streams<T>(kCache, D) && !kWindow, kRounded = rounds_weights<T>(kCache);
   static_assert(kRounded || !kExact, "one kind of sum");
   constexpr int kStepKeys = step_keys<T>();
   constexpr int kRegion = region_floats(D, kExact);
@@ -1398,8 +1495,8 @@ __global__ __launch_bounds__(kThreads, 2) void tva_tiled_kernel(TiledArgs a) {
 
   if (kDirect && a.status)
     for (int b = (int)(wg * kWaves + wv); b < a.batch; b += gridDim.x * kWaves)
-      smart::tva_validate_block_table(b, a.block_table, a.prefix_len, a.max_blocks, a.block_size, a.num_blocks, a.status,
-                                      lane);
+      smart::tva_validate_block_table<kWindow>(b, a.block_table, a.prefix_len, a.max_blocks, a.block_size, a.num_blocks, a.status, lane,
+                                               a.window, a.sinks);
 
   // Every wavefront plans for itself: what comes out is uniform over the workgroup.  Batches of more than 512 sequences are
   // summed by the eight wavefronts together (an eighth each) and searched in the eighth that holds what is looked for: a
@@ -1422,7 +1519,7 @@ __global__ __launch_bounds__(kThreads, 2) void tva_tiled_kernel(TiledArgs a) {
       before.units += s_part[k].units;
       before.segs += s_part[k].segs;
     }
-    scan_batch<T>(a, lane, c0, c1, &before, [&](int b0, bool, int64_t units, int64_t segs, int64_t eu, int64_t es) {
+    scan_batch<T, kWindow>(a, lane, c0, c1, &before, [&](int b0, bool, int64_t units, int64_t segs, int64_t eu, int64_t es) {
       const int64_t first = by_segment ? es : eu, count = by_segment ? segs : units;
       const uint64_t hit = __ballot(want >= first && want < first + count);
       if (hit) {
@@ -1442,7 +1539,7 @@ __global__ __launch_bounds__(kThreads, 2) void tva_tiled_kernel(TiledArgs a) {
   };
   if (divided) {
     Sums mine{};
-    scan_batch<T>(a, lane, first_chunk(wv), first_chunk(wv + 1), &mine, [](int, bool, int64_t, int64_t, int64_t, int64_t) {});
+    scan_batch<T, kWindow>(a, lane, first_chunk(wv), first_chunk(wv + 1), &mine, [](int, bool, int64_t, int64_t, int64_t, int64_t) {});
     if (lane == 0) s_part[wv] = mine;
     __syncthreads();
     Sums before{};
@@ -1453,9 +1550,9 @@ __global__ __launch_bounds__(kThreads, 2) void tva_tiled_kernel(TiledArgs a) {
       all.steps += s_part[k].steps;
       all.flags |= s_part[k].flags;
     }
-    if (!kDirect && wg == 0) scan_batch<T>(a, lane, first_chunk(wv), first_chunk(wv + 1), &before, keep_plan);
+    if (!kDirect && wg == 0) scan_batch<T, kWindow>(a, lane, first_chunk(wv), first_chunk(wv + 1), &before, keep_plan);
   } else if (!kDirect) {
-    scan_batch<T>(a, lane, 0, chunks, &all, keep_plan);
+    scan_batch<T, kWindow>(a, lane, 0, chunks, &all, keep_plan);
   }
   if (kDirect) {
     const int flags = find(wg, true);
@@ -1476,7 +1573,7 @@ __global__ __launch_bounds__(kThreads, 2) void tva_tiled_kernel(TiledArgs a) {
 
   if (at.b >= 0) {
     int b = at.b;
-    Shape sh = shape_of<T>(a, a.prefix_len[b], a.cu_nodes[b], a.cu_nodes[b + 1]);
+    Shape sh = shape_of<T, kWindow>(a, a.prefix_len[b], a.cu_nodes[b], a.cu_nodes[b + 1]);
     while (u0 < u1) {
       // on to the next sequence with units
       while (!kDirect && u0 >= at.units_before + a.Hkv * sh.head) {
@@ -1484,7 +1581,7 @@ __global__ __launch_bounds__(kThreads, 2) void tva_tiled_kernel(TiledArgs a) {
         at.segs_before += (int64_t)a.Hkv * sh.groups;
         ++b;
         if (b >= a.batch) return;
-        sh = shape_of<T>(a, a.prefix_len[b], a.cu_nodes[b], a.cu_nodes[b + 1]);
+        sh = shape_of<T, kWindow>(a, a.prefix_len[b], a.cu_nodes[b], a.cu_nodes[b + 1]);
       }
       int g, group, t0, t1;
       if (kDirect) {
@@ -1545,28 +1642,34 @@ __global__ __launch_bounds__(kThreads, 2) void tva_tiled_kernel(TiledArgs a) {
         st.put(regions + wv * kRegion, lane);
       } else {
         Rows<T, kPlain, D> rowset;
-        rowset.begin(a, sh.base, g, row0 + (busy ? rt * kRowTile : 0), rows, lane);
+        Span<kWindow> span;
+        int tokens = 0;
+        if constexpr (kWindow) {
+          tokens = __builtin_amdgcn_readfirstlane(length_of(a, b));
+          span = span_of<kWindow>(a, tokens);
+        }
+        rowset.begin(a, span, tokens, sh.base, sh.n, g, row0 + (busy ? rt * kRowTile : 0), rows, lane);
         Stage st;
         if (t0 < t1) {
-          st.load_ids(a, table, t0, len, tid);
-          st.load(a, t0, len, g, tid);
-          if (t0 + 1 < t1) st.load_ids(a, table, t0 + 1, len, tid);
+          st.load_ids(a, span, table, t0, len, tid);
+          st.load(a, span, t0, len, g, tid);
+          if (t0 + 1 < t1) st.load_ids(a, span, table, t0 + 1, len, tid);
         }
         __syncthreads();  // the piece before is done with the LDS
         for (int t = t0; t < t1; ++t) {
           uintx4* stage = lds + (t & 1) * (2 * Stage::kStepChunks);
           st.store(stage, tid, len - t * kStepKeys);
           if (t + 1 < t1) {
-            st.load(a, t + 1, len, g, tid);
-            if (t + 2 < t1) st.load_ids(a, table, t + 2, len, tid);
+            st.load(a, span, t + 1, len, g, tid);
+            if (t + 2 < t1) st.load_ids(a, span, table, t + 2, len, tid);
           }
           __syncthreads();  // the stage is full, and everyone is done with the other one
           if (busy)
             for (int x = first; x < kTilesPerStep; x += shared) {
               const int n_valid = len - t * kStepKeys - x * Stage::kKeys;
               if (n_valid <= 0) break;
-              rowset.template tile<kCache == kSameType, kRounded, kExact>(stage + x * Stage::kTileChunks, stage + Stage::kStepChunks + x * Stage::kTileChunks, n_valid,
-                                          a.c_stored, lane);
+              rowset.template tile<kCache == kSameType, kRounded, kExact, kWindow>(stage + x * Stage::kTileChunks, stage + Stage::kStepChunks + x * Stage::kTileChunks,
+                                          n_valid, len - n_valid, a.sinks, a.c_stored, lane);
             }
         }
         // fold: the states that share a row tile, in wavefront order
@@ -1616,9 +1719,9 @@ __global__ __launch_bounds__(kThreads, 2) void tva_tiled_kernel(TiledArgs a) {
           const bool active = i < group_rows;
           const int rho = row0 + (active ? i : 0);
           const int node = sh.base + rho / a.G, head = g * a.G + rho % a.G;
-          Finish<T, D, kExact> f;
+          Finish<T, D, kExact, kWindow> f;
           f.request(a, node, head, active, e);
-          f.tree(a, g, sh.base, kStream ? 0 : sh.n, e);
+          f.tree(a, g, sh.base, kStream ? 0 : sh.n, b, e);
           if (active && (kStream || t0 < t1))
             f.merge(f.fetch(s_ml[0][i] * a.m_scale, s_ml[1][i], s_ml[kExact ? 2 : 1][i], regions + (i >> 5) * kRegion + (i & 31) * 4, kRowTile * 4, e),
                     a.c);
@@ -1638,13 +1741,13 @@ __global__ __launch_bounds__(kThreads, 2) void tva_tiled_kernel(TiledArgs a) {
     for (int64_t node = wg; node < a.total_nodes; node += gridDim.x) {
       if (all.flags == 0 && node >= first_node && node < end_node) continue;
       const int b = owner_of(a, (int)node);
-      const Shape sh = shape_of<T>(a, a.prefix_len[b], a.cu_nodes[b], a.cu_nodes[b + 1]);
+      const Shape sh = shape_of<T, kWindow>(a, a.prefix_len[b], a.cu_nodes[b], a.cu_nodes[b + 1]);
       const bool owned = node >= sh.base && node - sh.base < sh.n;
       if (owned && ascending) continue;
       const int e = tid & (kCombineLanes - 1);
       for (int h0 = 0; h0 < a.Hq; h0 += kThreads / kCombineLanes) {
         const int h = h0 + tid / kCombineLanes;
-        if (owned) Finish<T, D, kExact>::walk(a, node * a.Hq + min(h, a.Hq - 1), h < a.Hq, e);
+        if (owned) Finish<T, D, kExact, kWindow>::walk(a, node * a.Hq + min(h, a.Hq - 1), h < a.Hq, e);
         else if (h < a.Hq) zero_row<T, D>(a, node * a.Hq + h, e);
       }
     }
@@ -1657,7 +1760,7 @@ __global__ __launch_bounds__(kThreads, 2) void tva_tiled_kernel(TiledArgs a) {
 // partials, merged by the first in a fixed order; for launches that leave wavefront slots idle (see finish_parts).
 // kParts = 0: a wavefront per eight rows goes through both.
 constexpr int finish_waves(int parts) { return parts > 0 ? 1 + parts : 4; }
-template <typename T, int D, int kParts, bool kExact>
+template <typename T, int D, int kParts, bool kExact, bool kWindow>
 __global__ __launch_bounds__(finish_waves(kParts) * kWave, kParts == 0 ? 2 : 1) void tva_tiled_finish_kernel(TiledArgs a) {
   constexpr int kRows = kWave / kCombineLanes, K4 = D / 32;
   constexpr int kStates = kParts > 0 ? kParts : 1;
@@ -1669,15 +1772,15 @@ __global__ __launch_bounds__(finish_waves(kParts) * kWave, kParts == 0 ? 2 : 1) 
   const int64_t wave = (int64_t)blockIdx.x * finish_waves(kParts) + wv;
   if (a.status)
     for (int64_t b = wave; b < a.batch; b += (int64_t)gridDim.x * finish_waves(kParts))
-      smart::tva_validate_block_table((int)b, a.block_table, a.prefix_len, a.max_blocks, a.block_size, a.num_blocks,
-                                      a.status, lane);
+      smart::tva_validate_block_table<kWindow>((int)b, a.block_table, a.prefix_len, a.max_blocks, a.block_size, a.num_blocks,
+                                               a.status, lane, a.window, a.sinks);
   const int64_t n_rows = (int64_t)a.total_nodes * a.Hq, first = (kParts > 0 ? (int64_t)blockIdx.x : wave) * kRows;
   if (first >= n_rows) return;
   const int64_t row_raw = first + lane / kCombineLanes;
   const bool there = row_raw < n_rows;
   const int64_t row = there ? row_raw : n_rows - 1;
   const int node = (int)(row / a.Hq), head = (int)(row % a.Hq), g = head / a.G;
-  Finish<T, D, kExact> f;
+  Finish<T, D, kExact, kWindow> f;
   if (part < 0) f.request(a, node, head, there, e);
   else f.clear();
   const int64_t U = a.plan[0], W = a.plan[1];
@@ -1695,10 +1798,10 @@ __global__ __launch_bounds__(finish_waves(kParts) * kWave, kParts == 0 ? 2 : 1) 
     b = owner_of(a, node);
   }
   if (U < 0) b = owner_of(a, node);  // offsets that are not ascending
-  const Shape sh = shape_of<T>(a, a.prefix_len[b], a.cu_nodes[b], a.cu_nodes[b + 1]);
+  const Shape sh = shape_of<T, kWindow>(a, a.prefix_len[b], a.cu_nodes[b], a.cu_nodes[b + 1]);
   const bool owned = there && node >= sh.base && (int64_t)node - sh.base < sh.n;
   const int64_t units_before = a.plan[2 + b], segs_before = a.plan[2 + a.batch + b];
-  if (part < 0) f.tree(a, g, sh.base, owned && !(a.stream && sh.steps > 0) ? sh.n : 0, e);
+  if (part < 0) f.tree(a, g, sh.base, owned && !(a.stream && sh.steps > 0) ? sh.n : 0, b, e);
   if ((kParts == 0 || part >= 0) && owned && sh.steps > 0 && U > 0) {
     const int rho = (node - sh.base) * a.G + head % a.G;
     const int group = rho / kGroupRows, r = rho % kGroupRows, local = g * sh.groups + group;
@@ -1733,7 +1836,7 @@ __global__ __launch_bounds__(finish_waves(kParts) * kWave, kParts == 0 ? 2 : 1) 
     if (part >= 0) return;
 #pragma unroll
     for (int p = 0; p < kParts; ++p) {
-      typename Finish<T, D, kExact>::Partial x;
+      typename Finish<T, D, kExact, kWindow>::Partial x;
       x.m = s_m[p][lane / kCombineLanes];
       x.l = s_l[p][lane / kCombineLanes];
       x.exact = kExact ? s_exact[kExact ? p : 0][lane / kCombineLanes] : 0.f;
@@ -1808,25 +1911,61 @@ static int32_t segment_cost(const tva_params& p, int32_t workgroups) {
 // (720 53.5 / 51.0, 756 27.0 / 28.3, 832 44.0 / 42.5); 1500, 16 sequences of 60 .. 128 nodes, 31.9 / 34.6 / 42.7; 2016 42.2 /
 // 47.7 / 70.6; the bf16 workload above (2176) 95.2 / 97.1 / 117.6.
 static int finish_parts(int64_t rows8) { return rows8 <= 128 ? 7 : (rows8 <= 640 ? 1 : 0); }
-template <typename T, int D, bool kExact>
+template <typename T, int D, bool kExact, bool kWindow>
 static void launch_finish(const TiledArgs& a, int64_t rows8, hipStream_t stream) {
   const int parts = finish_parts(rows8), waves = finish_waves(parts);
   const dim3 grid((unsigned)(parts > 0 ? rows8 : (rows8 + waves - 1) / waves)), block(waves * kWave);
-  if (parts == 7) hipLaunchKernelGGL((tva_tiled_finish_kernel<T, D, 7, kExact>), grid, block, 0, stream, a);
-  else if (parts == 1) hipLaunchKernelGGL((tva_tiled_finish_kernel<T, D, 1, kExact>), grid, block, 0, stream, a);
-  else hipLaunchKernelGGL((tva_tiled_finish_kernel<T, D, 0, kExact>), grid, block, 0, stream, a);
+  if (parts == 7) hipLaunchKernelGGL((tva_tiled_finish_kernel<T, D, 7, kExact, kWindow>), grid, block, 0, stream, a);
+  else if (parts == 1) hipLaunchKernelGGL((tva_tiled_finish_kernel<T, D, 1, kExact, kWindow>), grid, block, 0, stream, a);
+  else hipLaunchKernelGGL((tva_tiled_finish_kernel<T, D, 0, kExact, kWindow>), grid, block, 0, stream, a);
 }
 
-template <typename T, CacheType kCache, bool kPlain, int D, bool kExact = false>
+template <typename T, CacheType kCache, bool kPlain, int D, bool kWindow, bool kExact = false>
 static hipError_t launch_tiled(const TiledArgs& a, bool direct, unsigned grid, hipStream_t stream) {
   if (direct)
-    hipLaunchKernelGGL((tva_tiled_kernel<T, kCache, kPlain, D, true, kExact>), dim3(grid), dim3(kThreads), 0, stream, a);
+    hipLaunchKernelGGL((tva_tiled_kernel<T, kCache, kPlain, D, true, kExact, kWindow>), dim3(grid), dim3(kThreads), 0, stream, a);
   else
-    hipLaunchKernelGGL((tva_tiled_kernel<T, kCache, kPlain, D, false, kExact>), dim3(grid), dim3(kThreads), 0, stream, a);
+    hipLaunchKernelGGL((tva_tiled_kernel<T, kCache, kPlain, D, false, kExact, kWindow>), dim3(grid), dim3(kThreads), 0, stream, a);
   return hipGetLastError();
 }
 
-int32_t tva_launch_tiled(smart_ctx* ctx, hipStream_t stream, const tva_params& p, const TvaWorkspace* fixed) {
+// The kernels of a call, chosen by its types; the finishing one is split form only.
+template <bool kWindow>
+static hipError_t launch_prefix(const TiledArgs& a, bool f32, int D, bool exact, bool direct, unsigned grid, hipStream_t stream) {
+  hipError_t err = hipErrorInvalidValue;
+  const bool plain = a.plain;
+#define SMART_TILED(T, CACHE, PLAIN) \
+  err = D == 128 ? launch_tiled<T, CACHE, PLAIN, 128, kWindow>(a, direct, grid, stream) : launch_tiled<T, CACHE, PLAIN, 64, kWindow>(a, direct, grid, stream)
+  if (f32) {
+    if (a.fp4) SMART_TILED(float, kE2M1, false);
+    else if (a.fp8) { if (plain) SMART_TILED(float, kE4M3, true); else SMART_TILED(float, kE4M3, false); }
+    else { if (plain) SMART_TILED(float, kSameType, true); else SMART_TILED(float, kSameType, false); }
+  } else {
+    if (exact)
+      err = D == 128 ? launch_tiled<__bf16, kE2M1, false, 128, kWindow, true>(a, direct, grid, stream)
+                     : launch_tiled<__bf16, kE2M1, false, 64, kWindow, true>(a, direct, grid, stream);
+    else if (a.fp4) SMART_TILED(__bf16, kE2M1, false);
+    else if (a.fp8) { if (plain) SMART_TILED(__bf16, kE4M3, true); else SMART_TILED(__bf16, kE4M3, false); }
+    else { if (plain) SMART_TILED(__bf16, kSameType, true); else SMART_TILED(__bf16, kSameType, false); }
+  }
+#undef SMART_TILED
+  return err;
+}
+template <bool kWindow>
+static void launch_rest(const TiledArgs& a, bool f32, int D, bool exact, int64_t rows8, hipStream_t stream) {
+  if (f32) {
+    if (D == 128) launch_finish<float, 128, false, kWindow>(a, rows8, stream);
+    else launch_finish<float, 64, false, kWindow>(a, rows8, stream);
+  } else if (exact) {
+    if (D == 128) launch_finish<__bf16, 128, true, kWindow>(a, rows8, stream);
+    else launch_finish<__bf16, 64, true, kWindow>(a, rows8, stream);
+  } else {
+    if (D == 128) launch_finish<__bf16, 128, false, kWindow>(a, rows8, stream);
+    else launch_finish<__bf16, 64, false, kWindow>(a, rows8, stream);
+  }
+}
+
+int32_t tva_launch_tiled(smart_ctx* ctx, hipStream_t stream, const tva_params& p, const TvaWorkspace* fixed, const TvaWindow* window) {
   const int G = p.num_q_heads / p.num_kv_heads;
   const bool fp8 = p.kv_cache_dtype == SMART_FP8_E4M3, fp4 = p.kv_cache_dtype == SMART_FP4_E2M1, f32 = p.dtype == SMART_F32;
   const int64_t segs = tiled_segments(p.batch, p.total_nodes, p.num_q_heads, p.num_kv_heads);
@@ -1847,7 +1986,8 @@ int32_t tva_launch_tiled(smart_ctx* ctx, hipStream_t stream, const tva_params& p
   // 18089); four such sequences 204 .. 465; fp32, 2 x 4 heads of 64, 397 .. 1218 (46 .. 54, 8165 .. 8500).
   // Lengths are on the device, so a wide table with hardly anything in it runs split: 4096 tokens wide, prefixes of one
   // token, 16-node trees, 14.7 .. 15.5 us in fp32 where the general kernel takes 12.8 .. 13.8; from 8 tokens on it is behind.
-  const int64_t longest = (int64_t)p.max_blocks_per_seq * p.block_size;
+  int64_t longest = (int64_t)p.max_blocks_per_seq * p.block_size;
+  if (window) longest = std::min(longest, (int64_t)window->window + window->sinks);
   const int64_t step = f32 ? step_keys<float>() : step_keys<__bf16>(), rows = (int64_t)p.total_nodes * G;
   // `segs` is what any offsets can make; trees much alike make `likely` (where the grid is larger, the surplus comes last: then
   // consecutive segments go to different L2s, or those of one L2 would have them all.  30 sequences, 8 kv heads, 8 nodes, 64 tokens 18.0
@@ -1865,7 +2005,7 @@ int32_t tva_launch_tiled(smart_ctx* ctx, hipStream_t stream, const tva_params& p
   // segments than likely, and the last ones wait for a compute unit.  Row tiles of trees a quarter above the mean: 1 .. 30 nodes, 2048 ..
   // 4096 tokens, 71 / 81.)  Head dim 64, whose steps take 8.4 ns a key and whose split form 4 us, counts as four tiles: 8 nodes, one
   // sequence, 517 tokens 13.9 / 13.2, 1030 14.2 / 17.5; 32 sequences, 130 15.5 / 10.4, 1030 24.4 / 18.6, 4100 54.2 / 49.5.
-  const bool stream4 = fp4 && !f32 && streams<__bf16>(kE2M1, p.head_dim);
+  const bool stream4 = fp4 && !f32 && streams<__bf16>(kE2M1, p.head_dim) && !window;
   const int64_t cus = ctx->num_cus > 0 ? ctx->num_cus : 256, mean_rows = (rows + p.batch - 1) / p.batch;
   const int64_t likely = (int64_t)p.batch * p.num_kv_heads * ((mean_rows + kGroupRows - 1) / kGroupRows);
   const int64_t larger = mean_rows + mean_rows / 4, tiles = larger <= kRowTile ? 1 : (larger <= 2 * kRowTile ? 2 : 4);
@@ -1920,6 +2060,8 @@ int32_t tva_launch_tiled(smart_ctx* ctx, hipStream_t stream, const tva_params& p
   // 44.1 / 38.5, 4 sequences of 2048 .. 4096 with 12 nodes 31.5 / 25.4, with 64 48.6 / 42.7.  14 .. 36 and 4 .. 14 in their place differ by
   // 2 % on average.
   if (stream4) a.segment_cost = 20, a.tree_cost = 8;
+  a.window = window ? window->window : 0;
+  a.sinks = window ? window->sinks : 0;
   a.fp8 = fp8;
   a.fp4 = fp4;
   a.stream = stream4;
@@ -1936,36 +2078,13 @@ int32_t tva_launch_tiled(smart_ctx* ctx, hipStream_t stream, const tva_params& p
   int32_t rc = profile_begin(ctx, stream);
   if (rc != SMART_OK) return rc;
   const unsigned grid = direct ? (unsigned)segs : (unsigned)tiled_workgroups(ctx);
-  const bool plain = a.plain;
-  hipError_t err = hipErrorInvalidValue;
-#define SMART_TILED(T, CACHE, PLAIN) \
-  err = p.head_dim == 128 ? launch_tiled<T, CACHE, PLAIN, 128>(a, direct, grid, stream) : launch_tiled<T, CACHE, PLAIN, 64>(a, direct, grid, stream)
-  if (f32) {
-    if (fp4) SMART_TILED(float, kE2M1, false);
-    else if (fp8) { if (plain) SMART_TILED(float, kE4M3, true); else SMART_TILED(float, kE4M3, false); }
-    else { if (plain) SMART_TILED(float, kSameType, true); else SMART_TILED(float, kSameType, false); }
-  } else {
-    if (exact)
-      err = p.head_dim == 128 ? launch_tiled<__bf16, kE2M1, false, 128, true>(a, direct, grid, stream)
-                              : launch_tiled<__bf16, kE2M1, false, 64, true>(a, direct, grid, stream);
-    else if (fp4) SMART_TILED(__bf16, kE2M1, false);
-    else if (fp8) { if (plain) SMART_TILED(__bf16, kE4M3, true); else SMART_TILED(__bf16, kE4M3, false); }
-    else { if (plain) SMART_TILED(__bf16, kSameType, true); else SMART_TILED(__bf16, kSameType, false); }
-  }
-#undef SMART_TILED
+  const hipError_t err = window ? launch_prefix<true>(a, f32, p.head_dim, exact, direct, grid, stream)
+                                : launch_prefix<false>(a, f32, p.head_dim, exact, direct, grid, stream);
   SMART_HIP_CHECK(err);
   rc = profile_end(ctx, stream);
   if (rc != SMART_OK || direct) return rc;
-  if (f32) {
-    if (p.head_dim == 128) launch_finish<float, 128, false>(a, rows8, stream);
-    else launch_finish<float, 64, false>(a, rows8, stream);
-  } else if (exact) {
-    if (p.head_dim == 128) launch_finish<__bf16, 128, true>(a, rows8, stream);
-    else launch_finish<__bf16, 64, true>(a, rows8, stream);
-  } else {
-    if (p.head_dim == 128) launch_finish<__bf16, 128, false>(a, rows8, stream);
-    else launch_finish<__bf16, 64, false>(a, rows8, stream);
-  }
+  if (window) launch_rest<true>(a, f32, p.head_dim, exact, rows8, stream);
+  else launch_rest<false>(a, f32, p.head_dim, exact, rows8, stream);
   SMART_HIP_CHECK(hipGetLastError());
   return SMART_OK;
 }
