@@ -913,8 +913,8 @@ int32_t prompt_attention_window(smart_ctx* ctx, void* stream, const prompt_param
  * rotary_dim odd or outside 2 .. head_dim; unknown dtype / pairing; base not
  * positive; eps not positive or not below 1e30; token strides smaller than a
  * token's row; results in place with another stride; pointers that are not
- * aligned to an element); SMART_EHIP.  Rows that are aligned to 16 bytes are
- * fastest.
+ * aligned to an element); SMART_EHIP.  Rows aligned to four elements, and a
+ * head_dim and rotary_dim that are multiples of 8, are fastest.
  * ------------------------------------------------------------------------- */
 typedef struct {
   int32_t dtype; /* SMART_F32 | SMART_BF16: q, k, weights and results share it */

@@ -580,9 +580,12 @@ PyObject* cache_extend(PyObject* const* a) {
     PyErr_SetString(PyExc_ValueError, "kv_cache_extend: total_cap is negative");
     throw Failed();
   }
-  auto rows = i32_rows(4, std::max<int64_t>(batch, 1), length);  // (one number in the last)
-  at::Tensor cu = fresh(length, at::kInt, {batch + 1}), slots = fresh(length, at::kLong, {cap}), new_count = rows[3].slice(0, 0, 1);
-  for (int i = 0; i < 3; ++i) rows[i] = rows[i].slice(0, 0, batch);
+  // one allocation for the numbers: offsets, three rows, the count
+  at::AutoDispatchBelowADInplaceOrView no_gradients;  // (of whole numbers; half of a view's time)
+  const int64_t p = whole_rows(batch), first = whole_rows((int64_t)batch + 1);
+  at::Tensor buf = fresh(length, at::kInt, {first + 3 * p + 1}), slots = fresh(length, at::kLong, {cap}), rows[3];
+  at::Tensor cu = buf.as_strided({(int64_t)batch + 1}, {1}, 0), new_count = buf.as_strided({1}, {1}, first + 3 * p);
+  for (int i = 0; i < 3; ++i) rows[i] = buf.as_strided({batch}, {1}, first + i * p);
   void* s = stream(&length);
   call("kv_cache_extend", [&] {
     return lib.cache_extend(ctx, s, batch, bs, blocks, num_blocks, address<int32_t>(length), address<int32_t>(more), address<int32_t>(held),
@@ -601,9 +604,10 @@ PyObject* cache_release(PyObject* const* a) {
   const int32_t batch = block_tensors({&length, &held, &released, finished ? finished : &length}, table, free, count),
                 blocks = extent32(table.size(1)), bs = integer32(a[7]), window = integer32(a[9]), sinks = integer32(a[10]),
                 free_cap = extent32(free.numel());
-  auto rows = i32_rows(5, std::max<int64_t>(batch, 1), length);
-  at::Tensor new_count = rows[4].slice(0, 0, 1);
-  for (int i = 0; i < 4; ++i) rows[i] = rows[i].slice(0, 0, batch);
+  at::AutoDispatchBelowADInplaceOrView no_gradients;
+  const int64_t p = whole_rows(batch);
+  at::Tensor buf = fresh(length, at::kInt, {4 * p + 1}), rows[4], new_count = buf.as_strided({1}, {1}, 4 * p);
+  for (int i = 0; i < 4; ++i) rows[i] = buf.as_strided({batch}, {1}, i * p);
   void* s = stream(&length);
   call("kv_cache_release", [&] {
     return lib.cache_release(ctx, s, batch, bs, blocks, window, sinks, address<int32_t>(length), address<int32_t>(held), address<int32_t>(released),

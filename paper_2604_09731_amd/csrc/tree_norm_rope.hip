@@ -9,6 +9,10 @@
 // The angles of a token are formed once a wavefront, a pair a lane, and handed round through LDS.  An angle is a count of quarter
 // turns in binary64 (a binary32 product loses the fast pairs' phase at positions in the tens of thousands); what is left of it behind
 // the whole quarters is off by 2^-26 of one in binary32, which sine and cosine in binary32 are taken of.
+// 16384 tokens of 32 / 8 heads of 128, bf16: 65 us, 5.2 TB/s, the rate of a copy.  Vectors of 8 bytes and a wavefront for every place
+// on the chip, which goes on to further tokens (kWavesPerCu): their registers leave five wavefronts a SIMD.  With vectors of 16 bytes,
+// which halve the moves, three: 100 us; two passes in flight 77; a wavefront for every token, which forms the pairs' rates anew, 78 ..
+// 156; two passes of 8-byte vectors 82, five 65.
 #include <math.h>
 
 #include "common.h"
@@ -18,6 +22,7 @@ namespace {
 constexpr int kWave = 64, kWaves = 4, kThreads = kWave * kWaves;
 constexpr int kMaxDim = 128, kMaxPairs = kMaxDim / 2;
 constexpr int kPasses = 4;
+constexpr int kWavesPerCu = 20;
 
 struct NormRopeArgs {
   const void* q;
@@ -59,14 +64,15 @@ __global__ __launch_bounds__(kThreads) void tree_norm_rope_kernel(NormRopeArgs a
   const bool there = u * 2 * V < a.D, turns = u * 2 * V < a.rot;
   const int first = there ? (turns && !a.interleaved ? u * V : u * 2 * V) : 0;
   const int second = there ? first + (turns && !a.interleaved ? half : V) : V;
-  float wq[2][V], wk[2][V];
+  Chunk wq[2], wk[2];  // (as they are in memory: half the registers)
 #pragma unroll
-  for (int i = 0; i < V; ++i) {
-    wq[0][i] = a.wq ? wide(((const T*)a.wq)[first + i]) : 1.f;
-    wq[1][i] = a.wq ? wide(((const T*)a.wq)[second + i]) : 1.f;
-    wk[0][i] = a.wk ? wide(((const T*)a.wk)[first + i]) : 1.f;
-    wk[1][i] = a.wk ? wide(((const T*)a.wk)[second + i]) : 1.f;
-  }
+  for (int j = 0; j < 2; ++j)
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const int d = (j == 0 ? first : second) + i;
+      wq[j].x[i] = a.wq ? ((const T*)a.wq)[d] : (T)1.f;
+      wk[j].x[i] = a.wk ? ((const T*)a.wk)[d] : (T)1.f;
+    }
   // quarter turns a position of pair `lane`
   const double rate = lane < half ? exp2(-(2.0 * (double)lane / (double)a.rot) * a.log2_base) * 0.63661977236758134308 : 0.0;
   const float mean = 1.f / (float)a.D;
@@ -137,7 +143,7 @@ __global__ __launch_bounds__(kThreads) void tree_norm_rope_kernel(NormRopeArgs a
 #pragma unroll
       for (int j = 0; j < 2; ++j)
 #pragma unroll
-        for (int i = 0; i < V; ++i) y[j][i] *= inv * (is_q ? wq[j][i] : wk[j][i]);
+        for (int i = 0; i < V; ++i) y[j][i] *= inv * wide(is_q ? wq[j].x[i] : wk[j].x[i]);
       Chunk z[2];
       if (a.interleaved) {
 #pragma unroll
@@ -166,7 +172,7 @@ __global__ __launch_bounds__(kThreads) void tree_norm_rope_kernel(NormRopeArgs a
 template <typename T, int V, int L>
 int32_t launch(NormRopeArgs a, int32_t num_cus, hipStream_t stream) {
   const int passes = (a.H + kWave / L - 1) / (kWave / L);
-  const int64_t waves = (int64_t)(num_cus > 0 ? num_cus : 256) * 32;
+  const int64_t waves = (int64_t)(num_cus > 0 ? num_cus : 256) * kWavesPerCu;
   // A wavefront to a pass while that leaves some of the chip's wavefronts over, else as many passes as share their angles.
   a.per = (int64_t)a.n_tokens * passes <= waves / 2 ? 1 : (passes + (passes + kPasses - 1) / kPasses - 1) / ((passes + kPasses - 1) / kPasses);
   a.chunks = (passes + a.per - 1) / a.per;
@@ -174,6 +180,12 @@ int32_t launch(NormRopeArgs a, int32_t num_cus, hipStream_t stream) {
   hipLaunchKernelGGL((tree_norm_rope_kernel<T, V, L>), dim3((unsigned)groups), dim3(kThreads), 0, stream, a);
   SMART_HIP_CHECK(hipGetLastError());
   return SMART_OK;
+}
+
+template <typename T>
+int32_t launch_type(const NormRopeArgs& a, bool vectors, int32_t num_cus, hipStream_t stream) {
+  if (!vectors) return launch<T, 1, 64>(a, num_cus, stream);
+  return a.D <= 64 ? launch<T, 4, 8>(a, num_cus, stream) : launch<T, 4, 16>(a, num_cus, stream);
 }
 
 int32_t check(const norm_rope_params& p) {
@@ -237,14 +249,8 @@ extern "C" int32_t tree_norm_rope(smart_ctx* ctx, void* stream, const norm_rope_
   if (prev != ctx->device) SMART_HIP_CHECK(hipSetDevice(ctx->device));
   hipStream_t s = (hipStream_t)stream;
   const int32_t cus = ctx->num_cus;
-  if (p.dtype == SMART_F32) {
-    if (!vectors_of(p, 4)) rc = launch<float, 1, 64>(a, cus, s);
-    else rc = p.head_dim <= 64 ? launch<float, 4, 8>(a, cus, s) : launch<float, 4, 16>(a, cus, s);
-  } else {
-    if (vectors_of(p, 8)) rc = p.head_dim <= 64 ? launch<__bf16, 8, 4>(a, cus, s) : launch<__bf16, 8, 8>(a, cus, s);
-    else if (vectors_of(p, 4)) rc = launch<__bf16, 4, 16>(a, cus, s);
-    else rc = launch<__bf16, 1, 64>(a, cus, s);
-  }
+  if (p.dtype == SMART_F32) rc = launch_type<float>(a, vectors_of(p, 4), cus, s);
+  else rc = launch_type<__bf16>(a, vectors_of(p, 4), cus, s);
   if (prev != ctx->device) (void)hipSetDevice(prev);
   return rc;
 }
