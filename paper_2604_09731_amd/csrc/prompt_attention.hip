@@ -211,6 +211,7 @@ struct Stage {
   __device__ void load(const T* kp, const T* vp, const PromptArgs& a, const Span<kWindow>& span, int key0, int len, int tid) {
     int token0 = key0;
     if constexpr (kWindow) {
+      asm volatile("" : "+v"(tid));  // (offsets are derived anew where they change, so that nothing of them lives in registers until there)
       const bool both = key0 < span.gap && key0 + kKeys > span.gap;
       token0 = both ? 0 : span.token(key0);
       if (both) place_both(a, span, key0, len, tid);
@@ -546,6 +547,7 @@ struct RowsBf16 {
           s[r][half] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[ks][half], q[r][ks], ks == 0 ? (floatx4)(0.f) : s[r][half], 0, 0, 0);
   }
   __device__ void mask(floatx4 (&s)[N][2], const Span<kWindow>& span, int key0, int lane) const {
+    if (kWindow) asm volatile("" : "+v"(lane));  // (as in load)
     const int at = key0 + 8 * (lane >> 4);
 #pragma unroll
     for (int r = 0; r < N; ++r)
@@ -739,26 +741,30 @@ __global__ __launch_bounds__(kWaves* kWave, D == 64 && N == 2 ? 3 : 2) void prom
       next_stage();
     }
   };
-  if (kWindow) edge(min(steps, last >= span.window ? (last - span.window) / S::kKeys + 1 : 0));  // where the windows begin
-  // Stages that all rows of the wavefront see whole.
+  // Stages that all rows of the wavefront see whole lie between (one loop of each kind: a second copy of the edges' takes registers
+  // that the loops do not have).
   const int whole = mine < rows ? (first + 1) / S::kKeys : 0;
-  while (t < whole) {
+  for (int pass = kWindow ? 0 : 1; pass < 2; ++pass) {
+    const int inside = pass == 1 ? whole : 0;
+    while (t < inside) {
 #pragma unroll
-    for (int part = 0; part < 2; ++part) {
-      x.softmax(pb, s, a.c, v, at, part);
-      if (part == 1) {
-        __syncthreads();
-        fill();
+      for (int part = 0; part < 2; ++part) {
+        x.softmax(pb, s, a.c, v, at, part);
+        if (part == 1) {
+          __syncthreads();
+          fill();
+        }
+        __builtin_amdgcn_s_setprio(1);
+        x.output(v, pb, k, part == 0 ? at : other, 1 - part);  // (behind the last stage of no use, but there to be read)
+        x.scores(s, k);
+        __builtin_amdgcn_s_setprio(0);
+        __builtin_amdgcn_sched_barrier(0);
       }
-      __builtin_amdgcn_s_setprio(1);
-      x.output(v, pb, k, part == 0 ? at : other, 1 - part);  // (behind the last stage of no use, but there to be read)
-      x.scores(s, k);
-      __builtin_amdgcn_s_setprio(0);
-      __builtin_amdgcn_sched_barrier(0);
+      next_stage();
     }
-    next_stage();
+    // where the windows begin; the diagonal and the prompt's end
+    edge(pass == 1 ? steps : min(steps, last >= span.window ? (last - span.window) / S::kKeys + 1 : 0));
   }
-  edge(steps);  // the diagonal and the prompt's end
   if (mine < rows) x.finish(a, base, g, mine, rows, lane);
 }
 
@@ -785,8 +791,17 @@ int32_t launch_rows(const PromptArgs& a, hipStream_t stream) {
 // 3690; head dim 64, 8 heads, one of 4096 34.6 / 46.1 / 74.0, 64 of 1 .. 300 14.7 / 11.7 / 14.9, 4 of 1024 .. 2048 26.4 / 34.3 / 52.4;
 // 32 heads, 4 of 4096 383 / 309 / 289.  (Two teams of wavefronts on one row tile, with half of the keys each, are ahead for a few
 // prompts of few heads only: one of 4096, 8 heads of 64, 27 for 35 us; one of 2048, 32 heads of 128, 51; 8262 tokens 212.)
+// With a window a tile of more tokens than a sixth of it (of 256 rows: than a 64th) streams too many keys that few of its rows see, and
+// nothing is longest: 64 rows for longer.  One prompt of 8192 tokens, 32 / 8 heads of 128, windows of 100, 500 and 2000, tiles of 64 / 128
+// / 256 rows: 43 / 51 / 61, 85 / 80 / 91, 187 / 141 / 149; 64 / 8 heads 82 / 76 / 99, 149 / 133 / 152, 362 / 273 / 270; 16384 tokens, window
+// 4096 2660 / 1947 / 1800; 8 / 8 heads of 64 11 / 18 / 31, 19 / 26 / 51, 37 / 47 / 88; 2048 tokens, 32 / 8 heads of 128, window 2000 26 /
+// 34 / 39.
 int tile_rows(const PromptArgs& a, bool f32) {
   const int64_t rows = (int64_t)a.total_tokens * a.Hq, cus = a.num_cus;
+  if (a.window > 0 && !f32) {
+    const int64_t reach = (int64_t)a.window * a.G;
+    return rows <= 256 * cus || reach < 6 * 128 ? 64 : (rows < 4 * 256 * cus || reach < 64 * 256 ? 128 : 256);
+  }
   return f32 || rows <= 192 * cus ? 64 : (rows < 4 * 256 * cus ? 128 : 256);
 }
 int tile_threads(int rows, bool f32, int D) { return f32 || (rows == 256 && D == 128) ? 512 : 256; }

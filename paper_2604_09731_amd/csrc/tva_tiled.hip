@@ -305,9 +305,10 @@ constexpr bool streams(CacheType cache, int D) {
 // the rounded ones, so that a row that one key dominates comes out as that key's value and equal values as they are, and a row is
 // off by 2 2^-8 of its weighted mean |V| at most, about what rounding the result may cost (2^-8 of it).  The log-sum-exp needs the
 // sums of the unrounded ones beside them; they are carried where it is asked for (kExact).
+// With a window all bf16 calls do.
 template <typename T>
-constexpr bool rounds_weights(CacheType cache) {
-  return cache == kE2M1 && sizeof(T) == 2;
+constexpr bool rounds_weights(CacheType cache, bool window) {
+  return (cache == kE2M1 || window) && sizeof(T) == 2;
 }
 
 template <typename T, CacheType kCache, bool kPlain, int D>
@@ -1480,7 +1481,7 @@ template <typename T, CacheType kCache, bool kPlain, int D, bool kDirect, bool k
 __global__ __launch_bounds__(kThreads, 2) void tva_tiled_kernel(TiledArgs a) {
   typedef Stager<T, kCache, kPlain, D> Stage;
   typedef Fp4Stream<kExact> Stream;
-  constexpr bool kStream = streams<T>(kCache, D) && !kWindow, kRounded = rounds_weights<T>(kCache);
+  constexpr bool kStream = streams<T>(kCache, D) && !kWindow, kRounded = rounds_weights<T>(kCache, kWindow);
   static_assert(kRounded || !kExact, "one kind of sum");
   constexpr int kStepKeys = step_keys<T>();
   constexpr int kRegion = region_floats(D, kExact);
@@ -1929,39 +1930,41 @@ static hipError_t launch_tiled(const TiledArgs& a, bool direct, unsigned grid, h
   return hipGetLastError();
 }
 
-// The kernels of a call, chosen by its types; the finishing one is split form only.
+// The kernels of a call, chosen by its types.  (With a window all bf16 calls carry both kinds of sums: fewer kernels.)
+template <typename T, CacheType kCache, bool kPlain, bool kWindow>
+static hipError_t launch_kind(const TiledArgs& a, int D, bool exact, bool direct, unsigned grid, hipStream_t stream) {
+  constexpr bool kBoth = rounds_weights<T>(kCache, kWindow);
+  if (kBoth && (exact || kWindow))
+    return D == 128 ? launch_tiled<T, kCache, kPlain, 128, kWindow, kBoth>(a, direct, grid, stream)
+                    : launch_tiled<T, kCache, kPlain, 64, kWindow, kBoth>(a, direct, grid, stream);
+  return D == 128 ? launch_tiled<T, kCache, kPlain, 128, kWindow, kBoth && kWindow>(a, direct, grid, stream)
+                  : launch_tiled<T, kCache, kPlain, 64, kWindow, kBoth && kWindow>(a, direct, grid, stream);
+}
+template <typename T, bool kWindow>
+static hipError_t launch_prefix(const TiledArgs& a, int D, bool exact, bool direct, unsigned grid, hipStream_t stream) {
+  if (a.fp4) return launch_kind<T, kE2M1, false, kWindow>(a, D, exact, direct, grid, stream);
+  if (a.fp8)
+    return a.plain ? launch_kind<T, kE4M3, true, kWindow>(a, D, exact, direct, grid, stream)
+                   : launch_kind<T, kE4M3, false, kWindow>(a, D, exact, direct, grid, stream);
+  return a.plain ? launch_kind<T, kSameType, true, kWindow>(a, D, exact, direct, grid, stream)
+                 : launch_kind<T, kSameType, false, kWindow>(a, D, exact, direct, grid, stream);
+}
 template <bool kWindow>
 static hipError_t launch_prefix(const TiledArgs& a, bool f32, int D, bool exact, bool direct, unsigned grid, hipStream_t stream) {
-  hipError_t err = hipErrorInvalidValue;
-  const bool plain = a.plain;
-#define SMART_TILED(T, CACHE, PLAIN) \
-  err = D == 128 ? launch_tiled<T, CACHE, PLAIN, 128, kWindow>(a, direct, grid, stream) : launch_tiled<T, CACHE, PLAIN, 64, kWindow>(a, direct, grid, stream)
-  if (f32) {
-    if (a.fp4) SMART_TILED(float, kE2M1, false);
-    else if (a.fp8) { if (plain) SMART_TILED(float, kE4M3, true); else SMART_TILED(float, kE4M3, false); }
-    else { if (plain) SMART_TILED(float, kSameType, true); else SMART_TILED(float, kSameType, false); }
-  } else {
-    if (exact)
-      err = D == 128 ? launch_tiled<__bf16, kE2M1, false, 128, kWindow, true>(a, direct, grid, stream)
-                     : launch_tiled<__bf16, kE2M1, false, 64, kWindow, true>(a, direct, grid, stream);
-    else if (a.fp4) SMART_TILED(__bf16, kE2M1, false);
-    else if (a.fp8) { if (plain) SMART_TILED(__bf16, kE4M3, true); else SMART_TILED(__bf16, kE4M3, false); }
-    else { if (plain) SMART_TILED(__bf16, kSameType, true); else SMART_TILED(__bf16, kSameType, false); }
-  }
-#undef SMART_TILED
-  return err;
+  return f32 ? launch_prefix<float, kWindow>(a, D, exact, direct, grid, stream) : launch_prefix<__bf16, kWindow>(a, D, exact, direct, grid, stream);
 }
+// The finishing kernel of the split form.
 template <bool kWindow>
 static void launch_rest(const TiledArgs& a, bool f32, int D, bool exact, int64_t rows8, hipStream_t stream) {
   if (f32) {
     if (D == 128) launch_finish<float, 128, false, kWindow>(a, rows8, stream);
     else launch_finish<float, 64, false, kWindow>(a, rows8, stream);
-  } else if (exact) {
+  } else if (exact || kWindow) {
     if (D == 128) launch_finish<__bf16, 128, true, kWindow>(a, rows8, stream);
     else launch_finish<__bf16, 64, true, kWindow>(a, rows8, stream);
   } else {
-    if (D == 128) launch_finish<__bf16, 128, false, kWindow>(a, rows8, stream);
-    else launch_finish<__bf16, 64, false, kWindow>(a, rows8, stream);
+    if (D == 128) launch_finish<__bf16, 128, kWindow, kWindow>(a, rows8, stream);
+    else launch_finish<__bf16, 64, kWindow, kWindow>(a, rows8, stream);
   }
 }
 
@@ -2013,14 +2016,25 @@ int32_t tva_launch_tiled(smart_ctx* ctx, hipStream_t stream, const tva_params& p
   const bool few_steps = (longest <= step && rows <= 384 * (int64_t)p.batch) ||
                          (!f32 && longest <= 4 * step && rows <= 64 * (int64_t)p.batch);
   const bool few_steps4 = fp4 && !f32 && longest * (stream4 ? tiles : 4) * (5 * cus - 4 * (likely < cus ? likely : cus)) <= 2048 * 5 * cus;
-  bool direct = fixed != nullptr || (few_steps && fits) || (few_steps4 && fits4);
+  // With a window the longest segment is known: direct up to so many keys (of one, two, four row tiles, which take 11, 14 and 24 ns a
+  // key in bf16 and 26, 43 and 78 in fp32), and more the more of the chip the segments fill, 4 times at most (a few sequences may be long
+  // among short ones).  Split and direct, us.  bf16, head dim 128, 32 / 8 heads, windows of 250, 500, 1000, 2000 tokens: one sequence, 7
+  // nodes 16.6 / 16.6, 18.1 / 18.0, 19.6 / 23.9, 20.2 / 36.1; 16 nodes - / 20.6, - / 22.6, 23.4 / 30, 25.2 / 45; 8 sequences, 7 nodes
+  // - / 17.5, - / 19.2, 23.8 / 26.1, 28.2 / 38.2, 30 nodes 32.0 / 30.4, 32.5 / 36.1, 33.9 / 48.2, 40.4 / 72.2; 30 sequences, 7 nodes 30.4
+  // / 18.8, 32.4 / 22.4, 39.8 / 30.6, 55.5 / 46.8, 14 nodes 36.1 / 23.1, 39.0 / 26.1, 46.9 / 34.2, 65.0 / 50.7.  Head dim 64 breaks even a
+  // quarter later.  fp32, 64: one sequence, 7 nodes, 64, 128, 250 tokens 15.5 / 12.6, 15.5 / 14.3, 16.0 / 17.5; 30 sequences 24.0 / 13.8,
+  // 26.9 / 15.7, 30.1 / 19.9.
+  const int64_t cost = (mean_rows > kGroupRows ? 2 : 1) * (f32 ? (tiles == 1 ? 4 : (tiles == 2 ? 7 : 14)) : (tiles == 1 ? 4 : (tiles == 2 ? 5 : 10)));
+  const int64_t enough = f32 ? 560 : (p.head_dim == 128 ? 2400 : 3000), filled = std::min(4 * likely, (9 * cus) / 4);  // of 3 cus
+  const bool short_window = window && longest * cost * (3 * cus - filled) <= enough * 3 * cus;
+  bool direct = fixed != nullptr || (window ? short_window && fits4 : (few_steps && fits) || (few_steps4 && fits4));
   if (!direct) {
     hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
     if (stream != nullptr && hipStreamIsCapturing(stream, &capture) != hipSuccess) (void)hipGetLastError();
     direct = capture != hipStreamCaptureStatusNone;
   }
   void* ws = nullptr;
-  const bool exact = fp4 && !f32 && p.d_lse != nullptr;  // two kinds of sums (rounds_weights)
+  const bool exact = !f32 && (window || (fp4 && p.d_lse != nullptr));  // two kinds of sums (rounds_weights)
   const size_t partials = partials_bytes(ctx, segs, p.head_dim, exact);  // then the plan
   if (!direct) {
     const int32_t rc = tiled_workspace(ctx, stream, partials + plan_bytes(p.batch), &ws);
