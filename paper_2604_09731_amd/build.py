@@ -8,6 +8,7 @@ import os
 import subprocess
 import sys
 import sysconfig
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
@@ -16,6 +17,7 @@ LIB = os.path.join(HERE, "libsmart_tree.so")
 MARSHAL = os.path.join(HERE, "_marshal.so")
 TIMELINE_LIB = os.path.join(HERE, "libsmart_tree_timeline.so")
 TIMELINE_SOURCE = "tva_mfma.hip"        # the one source with stamps (-DSMART_TVA_TIMELINE)
+LONGEST_SOURCE = "tva_tiled.hip"
 OBJ_DIR = os.path.join(HERE, "_build")
 
 HIP_SOURCES = ["smart_ctx.hip", "tree_pack_accept.hip", "kv_cache_write.hip", "tva_general.hip",
@@ -59,23 +61,20 @@ def build_marshal(verbose: bool = False) -> str:
 
 def build_library(verbose: bool = False) -> str:
     os.makedirs(OBJ_DIR, exist_ok=True)
-    objs = []
-    for s in HIP_SOURCES:
-        o = os.path.join(OBJ_DIR, s + ".o")
-        _run([HIPCC, *HIP_FLAGS, *HIP_EXTRA.get(s, []), "-c", os.path.join(CSRC, s), "-o", o])
-        objs.append(o)
-    for s in HOST_SOURCES:
-        o = os.path.join(OBJ_DIR, s + ".o")
-        _run(["g++", *HOST_FLAGS, "-c", os.path.join(CSRC, s), "-o", o])
-        objs.append(o)
+    obj = lambda s: os.path.join(OBJ_DIR, s + ".o")
+    # the timeline build: one object compiled again with the stamps, the rest shared
+    plain, stamped = obj(TIMELINE_SOURCE), os.path.join(OBJ_DIR, TIMELINE_SOURCE + ".timeline.o")
+    steps = [[HIPCC, *HIP_FLAGS, *HIP_EXTRA.get(s, []), "-c", os.path.join(CSRC, s), "-o", obj(s)] for s in HIP_SOURCES]
+    steps += [[HIPCC, *HIP_FLAGS, "-DSMART_TVA_TIMELINE", "-c", os.path.join(CSRC, TIMELINE_SOURCE), "-o", stamped]]
+    steps += [["g++", *HOST_FLAGS, "-c", os.path.join(CSRC, s), "-o", obj(s)] for s in HOST_SOURCES]
+    with ThreadPoolExecutor(max_workers=min(6, os.cpu_count() or 1)) as pool:
+        # (one source with many kernels takes two minutes: it is first)
+        list(pool.map(_run, sorted(steps, key=lambda cmd: os.path.join(CSRC, LONGEST_SOURCE) not in cmd)))
+    objs = [obj(s) for s in HIP_SOURCES + HOST_SOURCES]
     _run([HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB, *objs, "-pthread"])
     if verbose:
         print("built", LIB)
     build_marshal(verbose)
-    # the timeline build: one object compiled again with the stamps, the rest shared
-    plain = os.path.join(OBJ_DIR, TIMELINE_SOURCE + ".o")
-    stamped = os.path.join(OBJ_DIR, TIMELINE_SOURCE + ".timeline.o")
-    _run([HIPCC, *HIP_FLAGS, "-DSMART_TVA_TIMELINE", "-c", os.path.join(CSRC, TIMELINE_SOURCE), "-o", stamped])
     _run([HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", TIMELINE_LIB,
           *[stamped if o == plain else o for o in objs], "-pthread"])
     if verbose:
