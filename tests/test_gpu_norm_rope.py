@@ -138,3 +138,18 @@ def test_captured_on_another_stream(lib):
         torch.cuda.synchronize()
         want = lib.tree_norm_rope(pos, q, k, *w)
         assert torch.equal(qo, want[0]) and torch.equal(ko, want[1])
+
+
+def test_tokens_that_lie_far_apart(lib):
+    import torch
+    T, stride = 700, 1 << 22
+    room = torch.empty((T - 1) * stride + 4096, dtype=torch.bfloat16, device="cuda")
+    q, k, w = _projection(T, 4, 2, 128, "bf16", 4)
+    far = lambda at, H: room.as_strided((T, H, 128), (stride, 128, 1), at)
+    qf, kf = far(0, 4), far(1024, 2)
+    qf.copy_(q)
+    kf.copy_(k)
+    pos = torch.arange(T, dtype=torch.int32, device="cuda")
+    want = lib.tree_norm_rope(pos, q, k, *w)
+    got = lib.tree_norm_rope(pos, qf, kf, *w, q_out=qf, k_out=kf)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])

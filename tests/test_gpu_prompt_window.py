@@ -140,3 +140,22 @@ def test_bad_offsets_write_nothing(lib):
         out = torch.full_like(q, 3.0)
         lib.prompt_attention(q, k, v, torch.tensor(offsets, dtype=torch.int32, device="cuda"), 0.125, out=out, window=5, sinks=1)
         assert (out == 3).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_tokens_that_lie_far_apart(lib, dtype):
+    """Offsets past 32 bits: where the first tokens and the window are more than that apart, the gap begins with a stage."""
+    import torch
+    dt, T, stride = (torch.bfloat16 if dtype == "bf16" else torch.float32), 1100, 1 << 22
+    room = torch.empty((T - 1) * stride + 4096, dtype=dt, device="cuda")
+    far = lambda at, H: room.as_strided((T, H, 64), (stride, 64, 1), at)
+    q, k, v = _inputs(T, 8, 2, 64, dtype, 41)
+    qf, kf, vf = far(0, 8), far(1024, 2), far(2048, 2)
+    for x, y in ((qf, q), (kf, k), (vf, v)):
+        x.copy_(y)
+    _, d_cu = _cu([T])
+    cu = np.array([0, T])
+    for window, sinks in ((100, 5), (64, 64), (300, 130)):
+        out, lse = lib.prompt_attention(qf, kf, vf, d_cu, 0.125, want_lse=True, window=window, sinks=sinks)
+        rows = [(0, t, h) for t in (0, 5, window, window + sinks, window + sinks + 64, 700, 1023, 1024, T - 1) for h in (0, 7)]
+        _check_rows(_f64(out), _f64(lse), _f64(q), _f64(k), _f64(v), cu, window, sinks, dtype, rows)

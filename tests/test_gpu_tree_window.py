@@ -295,3 +295,22 @@ def test_another_stream(lib):
         got = c.run(lib, want_lse=False)
     side.synchronize()
     assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("dtype,cache,layout", [("bf16", "same", "interleaved"), ("f32", "same", "plain"), ("bf16", "fp8", "plain")])
+def test_far_pages(lib, dtype, cache, layout):
+    """Pages whose offsets pass 32 bits, in a cache of more than 4 GiB."""
+    import torch
+    c = Case(lib, [400, 90], [6, 4], 150, 20, D=128, dtype=dtype, cache=cache, layout=layout, seed=21)
+    page = c.kc[0].numel()
+    nb, first = (5 << 30) // (page * c.kc.element_size()), len(c.kc)
+    far = []
+    for x in (c.kc, c.vc):
+        big = torch.empty((nb, *x.shape[1:]), dtype=x.dtype, device="cuda")
+        big[nb - first:] = x
+        far.append(big)
+    c.kc, c.vc = far
+    inside = (c.table >= 0) & (c.table < first)
+    c.table = torch.where(inside, c.table + (nb - first), torch.full_like(c.table, -1))
+    out, lse = c.run(lib)
+    c.check(out, lse)                       # (the prefixes are those of the near pages)
