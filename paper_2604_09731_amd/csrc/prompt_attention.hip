@@ -9,7 +9,11 @@
 //   * Row tiles are handed out from the longest down, of up to 64 prompts: what is dispatched last is short.
 //   * Bound by the matrix cores: 4 D flops per (row, key).
 //   * With a window (prompt_attention_window) a row tile streams the first tokens that stay visible and what the windows of its rows
-//     hold, as one axis without the gap between them (Span); every variant is compiled for both.
+//     hold, as one axis without the gap between them (Span); every variant is compiled for both.  16384 tokens, 64 / 8 heads of 128,
+//     window 4096 1.80 ms (1.07 PFLOP/s of what is seen, without a window 1.15); 5 prompts of 300 .. 5000, 32 / 8 heads, window 1024
+//     248 us (720 TFLOP/s; the same prompts without 420, 890): 17 stages a row tile, of which the masked ones at both ends and the
+//     tile's own beginning and end weigh more; fp32, 8 of 128 .. 1536, 8 / 2 heads of 64, window 200 34 us (61 TFLOP/s): four stages for
+//     218 keys, and 825 tiles on 512 places.
 //   * Values of later tokens are multiplied by probabilities of zero where a tile crosses the diagonal; a row that comes out
 //     infinite or NaN is evaluated once more over its own keys only (evaluate_again).
 #include <math.h>

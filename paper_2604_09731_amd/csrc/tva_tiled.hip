@@ -44,6 +44,17 @@
 // workgroups; finishing kernel 18); fp32 plain pages, batch 8, 8 / 2 heads of 64, prefixes of 128 .. 1536, 15-node trees
 // 778 -> 19 us, and its error against binary64 falls from 5.6e-7 to 3.1e-7 (shorter sums).
 //
+// With a window (tree_verify_attention_window) the same kernels run over the keys that some node sees, numbered without the gap behind
+// the first tokens (Span): a step's keys are eight tokens by eight wherever they lie, and the tiles at the ends of the gap are masked row
+// by row.  Every kernel is compiled for both, so that calls without a window keep their code.  bf16: 64 sequences, 64 / 8 heads of
+// 128, window 4096, one token each 202 us (1.08 GB, 5.3 TB/s); 32 sequences of 100 .. 8192 tokens, 4 .. 64 nodes, 32 / 8 heads, window 1024
+// 89 (prefix kernel 60, finishing 25: vector work, half of the prefix kernel's issue); one of 5000, 7 nodes, window 512, 19 (11 and 6,
+// chains of loads); fp8 in plain pages, 12 of 1500 .. 8192, 10 .. 24 nodes, 28 / 4 heads, window 2000, 40 (29 and 11).  Tried and
+// dropped: the tree as a last step of the prefix kernel (its registers make the streaming loop spill: the 64 sequences 287 us); a
+// finishing kernel with the tree staged in LDS (the wide trees 37 us instead of 25), or on the matrix cores with 32 rows a wavefront
+// (18, but 17 and 10 instead of 11 and 6 where the trees are small); pages addressed from 32-bit strides (a sixteenth of the prefix
+// kernel's vector instructions: 60 -> 58.5).
+//
 // The paper (Sec. 1) has the target model verify the tree in one forward pass; this is the attention sub-step.
 #include <math.h>
 
@@ -305,7 +316,7 @@ constexpr bool streams(CacheType cache, int D) {
 // the rounded ones, so that a row that one key dominates comes out as that key's value and equal values as they are, and a row is
 // off by 2 2^-8 of its weighted mean |V| at most, about what rounding the result may cost (2^-8 of it).  The log-sum-exp needs the
 // sums of the unrounded ones beside them; they are carried where it is asked for (kExact).
-// With a window all bf16 calls do.
+// With a window all bf16 calls do, as with prompts: 32 sequences, 4 .. 64 nodes, window 1024 93 -> 89 us, fp8, 12 sequences 44 -> 40.
 template <typename T>
 constexpr bool rounds_weights(CacheType cache, bool window) {
   return (cache == kE2M1 || window) && sizeof(T) == 2;
