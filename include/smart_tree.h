@@ -911,7 +911,7 @@ int32_t prompt_attention_window(smart_ctx* ctx, void* stream, const prompt_param
  * Host errors: SMART_EINVAL (null pointers, where there are heads; head counts
  * negative, both zero or together above 65535; head_dim odd or outside 2 .. 128;
  * rotary_dim odd or outside 2 .. head_dim; unknown dtype / pairing; base not
- * positive; eps not positive or not below 1e30; token strides smaller than a
+ * positive; eps below 2^-126 or not below 1e30; token strides smaller than a
  * token's row; results in place with another stride; pointers that are not
  * aligned to an element); SMART_EHIP.  Rows aligned to four elements, and a
  * head_dim and rotary_dim that are multiples of 8, are fastest.

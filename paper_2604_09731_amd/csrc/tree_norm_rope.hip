@@ -195,7 +195,7 @@ int32_t check(const norm_rope_params& p) {
   if (p.head_dim < 2 || p.head_dim > kMaxDim || p.head_dim % 2) return SMART_EINVAL;
   if (p.rotary_dim < 2 || p.rotary_dim > p.head_dim || p.rotary_dim % 2) return SMART_EINVAL;
   if (p.pairing != SMART_ROPE_HALF_SPLIT && p.pairing != SMART_ROPE_INTERLEAVED) return SMART_EINVAL;
-  if (!(p.base > 0.0) || !(p.base < 1e300) || !(p.eps > 0.f) || !(p.eps < 1e30f)) return SMART_EINVAL;
+  if (!(p.base > 0.0) || !(p.base < 1e300) || !(p.eps >= 0x1p-126f) || !(p.eps < 1e30f)) return SMART_EINVAL;
   const int64_t q_row = (int64_t)p.num_q_heads * p.head_dim, k_row = (int64_t)p.num_kv_heads * p.head_dim;
   if (p.q_stride < q_row || p.q_out_stride < q_row || p.k_stride < k_row || p.k_out_stride < k_row) return SMART_EINVAL;
   // (in place: a row where it was)

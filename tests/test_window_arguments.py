@@ -71,7 +71,7 @@ def _norm(**kw):
 @pytest.mark.parametrize("bad", [dict(dtype=2), dict(n_tokens=-1), dict(num_q_heads=-1), dict(num_q_heads=0, num_kv_heads=0), dict(num_kv_heads=65532, k_stride=1 << 23, k_out_stride=1 << 23),
                                  dict(head_dim=130), dict(head_dim=63), dict(head_dim=0), dict(rotary_dim=66), dict(rotary_dim=0), dict(rotary_dim=31),
                                  dict(pairing=2), dict(base=0.0), dict(base=float("nan")), dict(eps=0.0), dict(eps=-1.0), dict(eps=float("nan")),
-                                 dict(eps=1e30), dict(q_stride=255), dict(k_stride=127), dict(q_out_stride=255), dict(k_out_stride=64),
+                                 dict(eps=1e30), dict(eps=1e-40), dict(q_stride=255), dict(k_stride=127), dict(q_out_stride=255), dict(k_out_stride=64),
                                  dict(d_position=None), dict(d_q=None), dict(d_k=None), dict(d_q_out=None), dict(d_k_out=None), dict(d_q=AT + 1),
                                  dict(d_k_out=AT + 3), dict(d_q_weight=AT + 1), dict(dtype=B.SMART_F32, d_k_weight=AT + 2),
                                  dict(d_q_out=AT), dict(d_k_out=2 * AT)])
