@@ -979,9 +979,10 @@ int32_t tree_norm_rope(smart_ctx* ctx, void* stream, const norm_rope_params* par
  *                                0 .. held; such a sequence keeps what it has.
  * In both, free counts are taken within 0 .. free_cap, d_new_free_count[0] is the
  * new one, and results alias none of the numbers read.  No workspace.
- * Host errors: SMART_EINVAL (null pointers, negative sizes, block_size < 1,
- * max_blocks_per_seq * block_size or total_cap above 2^31 - 1, results that alias
- * the numbers; window or sinks negative, sinks without a window); SMART_EHIP.
+ * Host errors: SMART_EINVAL (null pointers, negative sizes, batch above 2^30,
+ * block_size < 1, max_blocks_per_seq * block_size or total_cap above 2^31 - 1,
+ * results that alias the numbers; window or sinks negative, sinks without a
+ * window); SMART_EHIP.
  * ------------------------------------------------------------------------- */
 int32_t kv_cache_extend(smart_ctx* ctx, void* stream, int32_t batch, int32_t block_size, int32_t max_blocks_per_seq,
                         int32_t num_blocks, const int32_t* d_len, const int32_t* d_new_tokens, const int32_t* d_held,

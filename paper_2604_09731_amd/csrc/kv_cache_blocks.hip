@@ -209,7 +209,8 @@ __global__ __launch_bounds__(kThreads) void kv_release_kernel(ReleaseArgs a) {
 }
 
 bool sizes_ok(int32_t batch, int32_t block_size, int32_t max_blocks, int32_t free_cap) {
-  return batch >= 0 && block_size > 0 && max_blocks >= 0 && free_cap >= 0 && (int64_t)max_blocks * block_size <= 0x7FFFFFFF;
+  // (batch: counted in int, 256 at a time)
+  return batch >= 0 && batch <= 1 << 30 && block_size > 0 && max_blocks >= 0 && free_cap >= 0 && (int64_t)max_blocks * block_size <= 0x7FFFFFFF;
 }
 
 // Workgroups for at most n rows: four rows a thread, and no more than fill the chip.

@@ -98,7 +98,7 @@ def _release(**kw):
     return B._lib().kv_cache_release(CTX, None, *dict(_RELEASE, **kw).values())
 
 
-@pytest.mark.parametrize("bad", [dict(batch=-1), dict(bs=0), dict(bs=-16), dict(width=-1), dict(width=1 << 28), dict(nb=-1), dict(cap=-1), dict(rows=-1),
+@pytest.mark.parametrize("bad", [dict(batch=-1), dict(batch=(1 << 30) + 1), dict(bs=0), dict(bs=-16), dict(width=-1), dict(width=1 << 28), dict(nb=-1), dict(cap=-1), dict(rows=-1),
                                  dict(rows=1 << 31), dict(length=None), dict(new=None), dict(held=None), dict(free=None), dict(count=None),
                                  dict(table=None), dict(cu=None), dict(slots=None), dict(new_length=None), dict(new_held=None), dict(new_count=None),
                                  dict(status=None), dict(new_count=5 * AT), dict(new_length=AT), dict(new_held=3 * AT), dict(status=2 * AT), dict(cu=AT)])
@@ -106,7 +106,7 @@ def test_extending(bad):
     assert _extend(**bad) == B.SMART_EINVAL
 
 
-@pytest.mark.parametrize("bad", [dict(batch=-1), dict(bs=0), dict(width=-1), dict(width=1 << 28), dict(window=-1), dict(sinks=-1),
+@pytest.mark.parametrize("bad", [dict(batch=-1), dict(batch=(1 << 30) + 1), dict(bs=0), dict(width=-1), dict(width=1 << 28), dict(window=-1), dict(sinks=-1),
                                  dict(window=0, sinks=1), dict(cap=-1), dict(length=None), dict(held=None), dict(released=None), dict(table=None),
                                  dict(free=None), dict(count=None), dict(new_length=None), dict(new_held=None), dict(new_released=None),
                                  dict(new_count=None), dict(status=None), dict(new_count=6 * AT), dict(new_length=AT), dict(new_held=2 * AT),
