@@ -17,7 +17,7 @@ def extend(length, new, held, table, free, count, block_size, num_blocks, cap):
             status.append(EINVAL)
             continue
         want = max(0, -(-(length[b] + n) // block_size) - held[b])
-        if length[b] + n > width * block_size or rows > cap:
+        if length[b] + n > width * block_size or (n and rows > cap):
             status.append(ECAP)
             continue
         if want and (short or want > count):

@@ -86,7 +86,7 @@ __global__ __launch_bounds__(kThreads) void kv_extend_kernel(ExtendArgs a) {
     const int64_t fresh = max(x.fresh, 0), end = (int64_t)x.len + fresh;
     int64_t chunk_rows, chunk_wanted;
     const int64_t row = rows + sum_before(fresh, lane, wv, s_sum[0], &chunk_rows);
-    const bool room = valid && end <= (int64_t)a.max_blocks * a.block_size && row + fresh <= a.total_cap;
+    const bool room = valid && end <= (int64_t)a.max_blocks * a.block_size && (fresh == 0 || row + fresh <= a.total_cap);
     const int64_t want = room ? max((int64_t)0, (end + a.block_size - 1) / a.block_size - x.held) : 0;
     const int64_t before = wanted + sum_before(want, lane, wv, s_sum[1], &chunk_wanted);
     const bool served = room && (want == 0 || before + want <= free_count);

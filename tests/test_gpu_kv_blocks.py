@@ -75,6 +75,11 @@ def test_numbers_that_do_not_fit(lib, length, new, held):
     _release(lib, [5, length, 0], [1, held, 0], [0, max(0, held) + 1, 0], [False, True, False], table, [9] * 6, 1, 8, 2, 0)
 
 
+def test_nothing_asked_behind_the_last_row(lib):
+    want = _extend(lib, [3, 4, 5, 8], [4, 9, 0, 1], [1, 1, 1, 1], [[1, -1, -1], [2, -1, -1], [3, -1, -1], [4, -1, -1]], [0, 5], 2, 8, 6, 6)
+    assert want[5] == [K.OK, K.ECAP, K.OK, K.ECAP]
+
+
 @pytest.mark.parametrize("count", [-5, 0, 1, 2, 3, 4, 99])
 def test_a_list_that_runs_short_or_over(lib, count):
     want = _extend(lib, [0, 8, 7, 0], [9, 0, 1, 1], [0, 1, 1, 0], [[-1] * 3, [4, -1, -1], [5, -1, -1], [-1] * 3], [0, 1, 2, 3], count, 8, 6, 11)

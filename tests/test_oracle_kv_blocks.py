@@ -42,6 +42,9 @@ def test_hand_worked():
     # the first takes block 3, the second lacks one of three, the third comes behind it and gets none either
     assert r == ([0, 3, 12, 13], [31, 12, 13] + [-1] * 17, [6, 0, 0], [2, 0, 0], 2, [K.OK, K.ECAP, K.ECAP])
     assert table[0] == [7, 3, -1]
+    # rows for the first only; the second keeps what it has, the third asks for nothing
+    assert K.extend([3, 4, 5], [4, 9, 0], [1, 1, 1], [[1, 0], [2, 0], [3, 0]], [], 0, 8, 6, 6) == (
+        [0, 4, 6, 6], [11, 12, 13, 14, -1, -1], [7, 4, 5], [1, 1, 1], 0, [K.OK, K.ECAP, K.OK])
     free = [9, -1, -1, -1, -1]
     r = K.release([40, 8], [5, 2], [0, 0], [False, True], [[1, 2, 3, 4, 5], [6, 7, 0, 0, 0]], free, 1, 8, 10, 3)
     # position 40 sees 31 ..: blocks 1 and 2 (tokens 8 .. 23) are behind it, block 0 holds the sinks
