@@ -1383,7 +1383,8 @@ struct Finish {
     int begins = 0;
     if constexpr (kWindow) {
       const int tokens = length_of(a, b);
-      span = span_of<kWindow>(a, tokens);
+      // (without a key, as where a window of 1 begins behind the last token, the loop's key 0 stays the table's first token)
+      if (sh.len > 0) span = span_of<kWindow>(a, tokens);
       begins = window_begin(a, span, tokens, node, sh.n);
     }
     constexpr int kAtOnce = 2;  // keys whose loads are in flight together (the last one again past the end)

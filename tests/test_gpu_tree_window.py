@@ -314,3 +314,18 @@ def test_far_pages(lib, dtype, cache, layout):
     c.table = torch.where(inside, c.table + (nb - first), torch.full_like(c.table, -1))
     out, lse = c.run(lib)
     c.check(out, lse)                       # (the prefixes are those of the near pages)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("batch", [20, 200])
+def test_windows_of_one_behind_full_tables(lib, dtype, batch):
+    """Single tokens that see themselves only: every row is its own value, an infinity too; the table has no entry behind the prefix."""
+    import torch
+    c = Case(lib, [59 + 5 * (b % 2) for b in range(batch)], [1] * batch, 1, 0, dtype=dtype, seed=batch)
+    c.table = c.table[:, :4].contiguous()
+    c.vt[batch // 2:, :, 5] = float("inf")
+    out, lse = c.run(lib)
+    assert torch.equal(out, c.vt.repeat_interleave(2, 1))
+    own = (c.q.double() * c.kt.double().repeat_interleave(2, 1)).sum(-1) * c.scale
+    S = (c.q.double() * c.kt.double().repeat_interleave(2, 1)).abs().sum(-1).max().item() * c.scale
+    assert (lse.double() - own).abs().max() <= ((2 * 64 + 2) * S + 34) * U + 2 * U * S
