@@ -5,14 +5,14 @@
 //
 // Bound by memory: each element is read and written once.  A head lies in L lanes of a wavefront, two vectors of V elements a
 // lane, which hold the two halves of V pairs, so that a pair is turned where it lies and a head's sum is a few moves between
-// neighbours.  A wavefront takes up to kPasses times 64 / L heads of one token, all of their loads in flight together.
+// neighbours.  A wavefront takes up to kPassesOf times 64 / L heads of one token, all of their loads in flight together.
 // The angles of a token are formed once a wavefront, a pair a lane, and handed round through LDS.  An angle is a count of quarter
 // turns in binary64 (a binary32 product loses the fast pairs' phase at positions in the tens of thousands); what is left of it behind
 // the whole quarters is off by 2^-26 of one in binary32, which sine and cosine in binary32 are taken of.
 // 16384 tokens of 32 / 8 heads of 128, bf16: 65 us, 5.2 TB/s, the rate of a copy.  Vectors of 8 bytes and a wavefront for every place
 // on the chip, which goes on to further tokens (kWavesPerCu): their registers leave five wavefronts a SIMD.  With vectors of 16 bytes,
 // which halve the moves, three: 100 us; two passes in flight 77; a wavefront for every token, which forms the pairs' rates anew, 78 ..
-// 156; two passes of 8-byte vectors 82, five 65.
+// 156; two passes of 8-byte vectors 82.
 #include <math.h>
 
 #include "common.h"
@@ -21,7 +21,10 @@ namespace {
 
 constexpr int kWave = 64, kWaves = 4, kThreads = kWave * kWaves;
 constexpr int kMaxDim = 128, kMaxPairs = kMaxDim / 2;
-constexpr int kPasses = 4;
+// Heads of fewer than 128 (lanes of a head idle) gain from more in flight: bf16, 16384 tokens of 40 heads of 64, 80, 96, 128, four and
+// five passes 31.0 / 28.8, 48.2 / 42.2, 53.5 / 51.3, 66 / 66 us; fp32, where five leave four wavefronts a SIMD, 68 / 70, 85 / 91, 99 / 103,
+// 131 / 131.
+template <typename T> constexpr int kPassesOf = sizeof(T) == 2 ? 5 : 4;
 constexpr int kWavesPerCu = 20;
 
 struct NormRopeArgs {
@@ -57,6 +60,7 @@ __device__ inline float sum_lanes(float x) {
 template <typename T, int V, int L>
 __global__ __launch_bounds__(kThreads) void tree_norm_rope_kernel(NormRopeArgs a) {
   typedef Vec<T, V> Chunk;
+  constexpr int kPasses = kPassesOf<T>;
   constexpr int kHeads = kWave / L;
   __shared__ float s_cos[kWaves][kMaxPairs], s_sin[kWaves][kMaxPairs];
   const int lane = threadIdx.x & (kWave - 1), wv = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
@@ -171,6 +175,7 @@ __global__ __launch_bounds__(kThreads) void tree_norm_rope_kernel(NormRopeArgs a
 
 template <typename T, int V, int L>
 int32_t launch(NormRopeArgs a, int32_t num_cus, hipStream_t stream) {
+  constexpr int kPasses = kPassesOf<T>;
   const int passes = (a.H + kWave / L - 1) / (kWave / L);
   const int64_t waves = (int64_t)(num_cus > 0 ? num_cus : 256) * kWavesPerCu;
   // A wavefront to a pass while that leaves some of the chip's wavefronts over, else as many passes as share their angles.
