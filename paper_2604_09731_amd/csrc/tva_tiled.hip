@@ -48,7 +48,7 @@
 // the first tokens (Span): a step's keys are eight tokens by eight wherever they lie, and the tiles at the ends of the gap are masked row
 // by row.  Every kernel is compiled for both, so that calls without a window keep their code.  bf16: 64 sequences, 64 / 8 heads of
 // 128, window 4096, one token each 202 us (1.08 GB, 5.3 TB/s); 32 sequences of 100 .. 8192 tokens, 4 .. 64 nodes, 32 / 8 heads, window 1024
-// 89 (prefix kernel 60, finishing 25: vector work, half of the prefix kernel's issue); one of 5000, 7 nodes, window 512, 19 (11 and 6,
+// 87 (prefix kernel 62, finishing 23: vector work, half of the prefix kernel's issue); one of 5000, 7 nodes, window 512, 19 (11 and 6,
 // chains of loads); fp8 in plain pages, 12 of 1500 .. 8192, 10 .. 24 nodes, 28 / 4 heads, window 2000, 40 (29 and 11).  Tried and
 // dropped: the tree as a last step of the prefix kernel (its registers make the streaming loop spill: the 64 sequences 287 us); a
 // finishing kernel with the tree staged in LDS (the wide trees 37 us instead of 25), or on the matrix cores with 32 rows a wavefront
@@ -1296,7 +1296,9 @@ struct Finish {
       }
     }
   }
-  // The tree part: the set bits of the row's ancestor mask, lowest first, of a tree of n nodes of sequence b.
+  // The tree part: the set bits of the row's ancestor mask, lowest first, of a tree of n nodes of sequence b.  kLean: without
+  // requesting the next keys while the last are used, in fewer registers.
+  template <bool kLean = false>
   __device__ void tree(const TiledArgs& a, int g, int base, int n, int b, int e) {
     limit(a, n, b);
     const T* kt = (const T*)a.k_tree + ((int64_t)base * a.Hkv + g) * D;
@@ -1304,7 +1306,12 @@ struct Finish {
     const int64_t node_stride = (int64_t)a.Hkv * D;
     Keys cur = next_keys(kt, vt, node_stride, e);
     while (__any(cur.have[0])) {
-      const Keys nxt = next_keys(kt, vt, node_stride, e);
+      Keys nxt;
+      if (!kLean) nxt = next_keys(kt, vt, node_stride, e);
+      if (kLean) {
+#pragma unroll
+        for (int k = 0; k < K4; ++k) asm volatile("" : "+v"(q[k]));  // (widened anew, not kept so)
+      }
       float dot[2];
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
@@ -1325,6 +1332,7 @@ struct Finish {
       m = m_new;
 #pragma unroll
       for (int k = 0; k < K4; ++k) acc[k] = acc[k] * al + (p0 * widen(cur.v[0][k]) + p1 * widen(cur.v[1][k]));
+      if (kLean) nxt = next_keys(kt, vt, node_stride, e);
       cur = nxt;
     }
   }
@@ -1371,6 +1379,7 @@ struct Finish {
   // The whole row again, key by key: the prefix, then the tree part, in binary32 products with probabilities of at most 1.
   // For rows that are hardly ever seen, so it is small and not fast: 2 us a key (one sequence of 16384 tokens whose values
   // hold an infinity 33 ms, the general kernel 13.4).
+  template <int kAtOnce = 2>  // keys whose loads are in flight together (the last one again past the end)
   __device__ static void walk(const TiledArgs& a, int64_t row, bool active, int e) {
     asm volatile("" : "+v"(row));  // everything is derived anew, so that nothing lives in registers until here
     const int node = (int)(row / a.Hq), head = (int)(row % a.Hq), g = head / a.G;
@@ -1387,7 +1396,6 @@ struct Finish {
       if (sh.len > 0) span = span_of<kWindow>(a, tokens);
       begins = window_begin(a, span, tokens, node, sh.n);
     }
-    constexpr int kAtOnce = 2;  // keys whose loads are in flight together (the last one again past the end)
     for (int t0 = 0; __any(t0 < len); t0 += kAtOnce) {
       floatx4 k4[kAtOnce][K4], v4[kAtOnce][K4];
 #pragma unroll
@@ -1773,8 +1781,14 @@ __global__ __launch_bounds__(kThreads, 2) void tva_tiled_kernel(TiledArgs a) {
 // partials, merged by the first in a fixed order; for launches that leave wavefront slots idle (see finish_parts).
 // kParts = 0: a wavefront per eight rows goes through both.
 constexpr int finish_waves(int parts) { return parts > 0 ? 1 + parts : 4; }
+// With a window a wavefront that goes through both chains keeps less in flight (the next tree keys, what its segment's place follows
+// from), which leaves four a SIMD instead of three: 32 sequences of 4 .. 64 nodes 25 -> 23 us (the call 83.5 -> 80), 96 of 1 .. 20, window
+// 500, the call 85 -> 81.5; 12 of 10 .. 24, fp8, 11.7 -> 12.0.  (Five, or four with all of it in flight, spill: 43 us for the 25.)
+template <typename T, int D>
+constexpr bool lean_finish(int parts, bool window) { return parts == 0 && window && D == 128 && sizeof(T) == 2; }
 template <typename T, int D, int kParts, bool kExact, bool kWindow>
-__global__ __launch_bounds__(finish_waves(kParts) * kWave, kParts == 0 ? 2 : 1) void tva_tiled_finish_kernel(TiledArgs a) {
+__global__ __launch_bounds__(finish_waves(kParts) * kWave, (lean_finish<T, D>(kParts, kWindow) ? 4 : kParts == 0 ? 2 : 1)) void tva_tiled_finish_kernel(TiledArgs a) {
+  constexpr bool kLean = lean_finish<T, D>(kParts, kWindow);
   constexpr int kRows = kWave / kCombineLanes, K4 = D / 32;
   constexpr int kStates = kParts > 0 ? kParts : 1;
   __shared__ floatx4 s_acc[kStates][K4][kWave];
@@ -1814,20 +1828,33 @@ __global__ __launch_bounds__(finish_waves(kParts) * kWave, kParts == 0 ? 2 : 1) 
   const Shape sh = shape_of<T, kWindow>(a, a.prefix_len[b], a.cu_nodes[b], a.cu_nodes[b + 1]);
   const bool owned = there && node >= sh.base && (int64_t)node - sh.base < sh.n;
   const int64_t units_before = a.plan[2 + b], segs_before = a.plan[2 + a.batch + b];
-  if (part < 0) f.tree(a, g, sh.base, owned && !(a.stream && sh.steps > 0) ? sh.n : 0, b, e);
-  if ((kParts == 0 || part >= 0) && owned && sh.steps > 0 && U > 0) {
+  // workers that hold a part of the row's segment, their slots' offset, and the row in its group
+  int w_first = 0, w_last = -1, first_slot = 0, r = 0;
+  auto locate = [&]() {
+    if (!((kParts == 0 || part >= 0) && owned && sh.steps > 0 && U > 0)) return;
     const int rho = (node - sh.base) * a.G + head % a.G;
-    const int group = rho / kGroupRows, r = rho % kGroupRows, local = g * sh.groups + group;
+    const int group = rho / kGroupRows;
+    r = rho % kGroupRows;
     // (a step belongs to the worker that holds its last unit)
     const int64_t ub = units_before + g * sh.head + group * sh.full;
     const int cost = group < sh.groups - 1 ? StepCost<T>::four : sh.cost_last;
-    const int64_t w_first = ((ub + cost) * W - 1) / U, w_last = ((ub + (int64_t)sh.steps * cost) * W - 1) / U;
-    auto partial = [&](int64_t w) {
-      const float* slot = a.ws + (w + segs_before + local) * slot_floats(D, kExact);
+    w_first = (int)(((ub + cost) * W - 1) / U);
+    w_last = (int)(((ub + (int64_t)sh.steps * cost) * W - 1) / U);
+    first_slot = (int)segs_before + g * sh.groups + group;
+  };
+  if (kLean) {
+    locate();
+    asm volatile("" : "+v"(w_first), "+v"(w_last), "+v"(first_slot), "+v"(r));  // (here, so that what they follow from is not kept)
+  }
+  if (part < 0) f.template tree<kLean>(a, g, sh.base, owned && !(a.stream && sh.steps > 0) ? sh.n : 0, b, e);
+  if (!kLean) locate();
+  if (w_first <= w_last) {
+    auto partial = [&](int w) {
+      const float* slot = a.ws + (int64_t)(w + first_slot) * slot_floats(D, kExact);
       return f.fetch(slot[kGroupRows * D + r], slot[kGroupRows * D + kGroupRows + r], kExact ? slot[kGroupRows * D + 2 * kGroupRows + r] : 0.f,
                      slot + r * 4, kGroupRows * 4, e);
     };
-    for (int64_t w = w_first + (kParts > 0 ? part : 0); w <= w_last; w += 2 * kStates) {
+    for (int w = w_first + (kParts > 0 ? part : 0); w <= w_last; w += 2 * kStates) {
       const auto p0 = partial(w);
       auto p1 = partial(min(w + kStates, w_last));  // (no branch around it: both are requested before the first is used)
       if (w + kStates > w_last) p1.m = -INFINITY;
@@ -1860,7 +1887,7 @@ __global__ __launch_bounds__(finish_waves(kParts) * kWave, kParts == 0 ? 2 : 1) 
   }
   if (owned) f.write(a, node, head, e);
   const bool again = (f.row_overflowed(lane) || U < 0) && owned;
-  if (__any(again)) f.walk(a, (int64_t)node * a.Hq + head, again, e);
+  if (__any(again)) f.template walk<kLean ? 1 : 2>(a, (int64_t)node * a.Hq + head, again, e);
   if (there && !owned) zero_row<T, D>(a, row, e);
 }
 
