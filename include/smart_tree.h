@@ -682,10 +682,10 @@ int32_t tree_verify_attention(smart_ctx* ctx, void* stream, const tva_params* pa
  * tokens or tokens from prefix_len - window + 1 on are used, and checked
  * (d_status): the others may have been given back (kv_cache_release).
  * Every element type, layout, head_dim, block_size and cache of
- * tree_verify_attention.  bf16 calls treat softmax weights as those on a 4-bit cache
- * do, whatever the cache: those of cached tokens are rounded to bf16, the divisor is
- * the sum of the rounded ones, lse that of the unrounded.  A call whose window
- * holds all that the table can is tree_verify_attention.  A captured call, and
+ * tree_verify_attention.  Softmax weights are held in fp32, on a 4-bit cache as
+ * tree_verify_attention holds them there.  A call whose window holds all that the
+ * table can is tree_verify_attention (where bf16 / interleaved / block_size 16 /
+ * head_dim 128 rounds the weights to bf16).  A captured call, and
  * one for which there is no memory, takes the workspace-free form described at
  * tree_verify_attention_static.
  * Host errors: as tree_verify_attention, plus SMART_EINVAL for window < 1 or

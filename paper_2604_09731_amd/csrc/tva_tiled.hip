@@ -316,10 +316,9 @@ constexpr bool streams(CacheType cache, int D) {
 // the rounded ones, so that a row that one key dominates comes out as that key's value and equal values as they are, and a row is
 // off by 2 2^-8 of its weighted mean |V| at most, about what rounding the result may cost (2^-8 of it).  The log-sum-exp needs the
 // sums of the unrounded ones beside them; they are carried where it is asked for (kExact).
-// With a window all bf16 calls do, as with prompts: 32 sequences, 4 .. 64 nodes, window 1024 93 -> 89 us, fp8, 12 sequences 44 -> 40.
 template <typename T>
-constexpr bool rounds_weights(CacheType cache, bool window) {
-  return (cache == kE2M1 || window) && sizeof(T) == 2;
+constexpr bool rounds_weights(CacheType cache) {
+  return cache == kE2M1 && sizeof(T) == 2;
 }
 
 template <typename T, CacheType kCache, bool kPlain, int D>
@@ -633,9 +632,10 @@ struct Rows<__bf16, kPlain, D> {
         if (key_of_row(8 * (r >> 2) + 4 * h + (r & 3)) >= n_valid) s[r] = -INFINITY;
     }
     if (kWindow && key0 + 32 > sinks && __any(key0 < begins)) {
+      asm volatile("" : "+v"(lane));  // (the rows' keys are derived anew: kept through the loop they and what they are compared with spill)
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
-        const int at = key_of_row(8 * (r >> 2) + 4 * h + (r & 3));
+        const int at = key_of_row(8 * (r >> 2) + 4 * (lane >> 5) + (r & 3));
         if (at >= sinks - key0 && at < begins - key0) s[r] = -INFINITY;
       }
     }
@@ -1501,7 +1501,7 @@ template <typename T, CacheType kCache, bool kPlain, int D, bool kDirect, bool k
 __global__ __launch_bounds__(kThreads, 2) void tva_tiled_kernel(TiledArgs a) {
   typedef Stager<T, kCache, kPlain, D> Stage;
   typedef Fp4Stream<kExact> Stream;
-  constexpr bool kStream = streams<T>(kCache, D) && !kWindow, kRounded = rounds_weights<T>(kCache, kWindow);
+  constexpr bool kStream = streams<T>(kCache, D) && !kWindow, kRounded = rounds_weights<T>(kCache);
   static_assert(kRounded || !kExact, "one kind of sum");
   constexpr int kStepKeys = step_keys<T>();
   constexpr int kRegion = region_floats(D, kExact);
@@ -1960,7 +1960,7 @@ static void launch_finish(const TiledArgs& a, int64_t rows8, hipStream_t stream)
   else hipLaunchKernelGGL((tva_tiled_finish_kernel<T, D, 0, kExact, kWindow>), grid, block, 0, stream, a);
 }
 
-template <typename T, CacheType kCache, bool kPlain, int D, bool kWindow, bool kExact = false>
+template <typename T, CacheType kCache, bool kPlain, int D, bool kExact, bool kWindow>
 static hipError_t launch_tiled(const TiledArgs& a, bool direct, unsigned grid, hipStream_t stream) {
   if (direct)
     hipLaunchKernelGGL((tva_tiled_kernel<T, kCache, kPlain, D, true, kExact, kWindow>), dim3(grid), dim3(kThreads), 0, stream, a);
@@ -1969,15 +1969,15 @@ static hipError_t launch_tiled(const TiledArgs& a, bool direct, unsigned grid, h
   return hipGetLastError();
 }
 
-// The kernels of a call, chosen by its types.  (With a window all bf16 calls carry both kinds of sums: fewer kernels.)
+// The kernels of a call, chosen by its types.
 template <typename T, CacheType kCache, bool kPlain, bool kWindow>
 static hipError_t launch_kind(const TiledArgs& a, int D, bool exact, bool direct, unsigned grid, hipStream_t stream) {
-  constexpr bool kBoth = rounds_weights<T>(kCache, kWindow);
-  if (kBoth && (exact || kWindow))
-    return D == 128 ? launch_tiled<T, kCache, kPlain, 128, kWindow, kBoth>(a, direct, grid, stream)
-                    : launch_tiled<T, kCache, kPlain, 64, kWindow, kBoth>(a, direct, grid, stream);
-  return D == 128 ? launch_tiled<T, kCache, kPlain, 128, kWindow, kBoth && kWindow>(a, direct, grid, stream)
-                  : launch_tiled<T, kCache, kPlain, 64, kWindow, kBoth && kWindow>(a, direct, grid, stream);
+  constexpr bool kBoth = rounds_weights<T>(kCache);
+  if (kBoth && exact)
+    return D == 128 ? launch_tiled<T, kCache, kPlain, 128, kBoth, kWindow>(a, direct, grid, stream)
+                    : launch_tiled<T, kCache, kPlain, 64, kBoth, kWindow>(a, direct, grid, stream);
+  return D == 128 ? launch_tiled<T, kCache, kPlain, 128, false, kWindow>(a, direct, grid, stream)
+                  : launch_tiled<T, kCache, kPlain, 64, false, kWindow>(a, direct, grid, stream);
 }
 template <typename T, bool kWindow>
 static hipError_t launch_prefix(const TiledArgs& a, int D, bool exact, bool direct, unsigned grid, hipStream_t stream) {
@@ -1998,12 +1998,12 @@ static void launch_rest(const TiledArgs& a, bool f32, int D, bool exact, int64_t
   if (f32) {
     if (D == 128) launch_finish<float, 128, false, kWindow>(a, rows8, stream);
     else launch_finish<float, 64, false, kWindow>(a, rows8, stream);
-  } else if (exact || kWindow) {
+  } else if (exact) {
     if (D == 128) launch_finish<__bf16, 128, true, kWindow>(a, rows8, stream);
     else launch_finish<__bf16, 64, true, kWindow>(a, rows8, stream);
   } else {
-    if (D == 128) launch_finish<__bf16, 128, kWindow, kWindow>(a, rows8, stream);
-    else launch_finish<__bf16, 64, kWindow, kWindow>(a, rows8, stream);
+    if (D == 128) launch_finish<__bf16, 128, false, kWindow>(a, rows8, stream);
+    else launch_finish<__bf16, 64, false, kWindow>(a, rows8, stream);
   }
 }
 
@@ -2055,12 +2055,12 @@ int32_t tva_launch_tiled(smart_ctx* ctx, hipStream_t stream, const tva_params& p
   const bool few_steps = (longest <= step && rows <= 384 * (int64_t)p.batch) ||
                          (!f32 && longest <= 4 * step && rows <= 64 * (int64_t)p.batch);
   const bool few_steps4 = fp4 && !f32 && longest * (stream4 ? tiles : 4) * (5 * cus - 4 * (likely < cus ? likely : cus)) <= 2048 * 5 * cus;
-  // With a window the longest segment is known: direct up to so many keys (of one, two, four row tiles, which take 11, 14 and 24 ns a
+  // With a window the longest segment is known: direct up to so many keys (of one, two, four row tiles, which take 14, 18 and 31 ns a
   // key in bf16 and 26, 43 and 78 in fp32), and more the more of the chip the segments fill, 4 times at most (a few sequences may be long
-  // among short ones).  Split and direct, us.  bf16, head dim 128, 32 / 8 heads, windows of 250, 500, 1000, 2000 tokens: one sequence, 7
-  // nodes 16.6 / 16.6, 18.1 / 18.0, 19.6 / 23.9, 20.2 / 36.1; 16 nodes - / 20.6, - / 22.6, 23.4 / 30, 25.2 / 45; 8 sequences, 7 nodes
-  // - / 17.5, - / 19.2, 23.8 / 26.1, 28.2 / 38.2, 30 nodes 32.0 / 30.4, 32.5 / 36.1, 33.9 / 48.2, 40.4 / 72.2; 30 sequences, 7 nodes 30.4
-  // / 18.8, 32.4 / 22.4, 39.8 / 30.6, 55.5 / 46.8, 14 nodes 36.1 / 23.1, 39.0 / 26.1, 46.9 / 34.2, 65.0 / 50.7.  Head dim 64 breaks even a
+  // among short ones).  Split and direct, us.  bf16, head dim 128, 32 / 8 heads, prefixes of 3500, windows of 250, 500, 1000, 2000 tokens: one
+  // sequence, 7 nodes 17.6 / 15.0, 18.0 / 18.5, 18.6 / 25.2, 19.4 / 38.8; 16 nodes 20.7 / 19.4, 21.9 / 24.1, 22.9 / 33.3, 25 / 52; 8
+  // sequences, 7 nodes 20.3 / 15.9, 21.5 / 19.5, 23.5 / 27, 28 / 41, 30 nodes 32.5 / 32, 34.5 / 41, 37 / 57, 46 / 86; 30 sequences, 7 nodes
+  // 29.5 / 17.3, 33.5 / 23, 41.5 / 31.5, 57 / 48, 14 nodes 35.5 / 22.7, 40.5 / 28.8, 51 / 39, 72 / 62.  Head dim 64 breaks even a
   // quarter later.  fp32, 64: one sequence, 7 nodes, 64, 128, 250 tokens 15.5 / 12.6, 15.5 / 14.3, 16.0 / 17.5; 30 sequences 24.0 / 13.8,
   // 26.9 / 15.7, 30.1 / 19.9.
   const int64_t cost = (mean_rows > kGroupRows ? 2 : 1) * (f32 ? (tiles == 1 ? 4 : (tiles == 2 ? 7 : 14)) : (tiles == 1 ? 4 : (tiles == 2 ? 5 : 10)));
@@ -2073,7 +2073,7 @@ int32_t tva_launch_tiled(smart_ctx* ctx, hipStream_t stream, const tva_params& p
     direct = capture != hipStreamCaptureStatusNone;
   }
   void* ws = nullptr;
-  const bool exact = !f32 && (window || (fp4 && p.d_lse != nullptr));  // two kinds of sums (rounds_weights)
+  const bool exact = fp4 && !f32 && p.d_lse != nullptr;  // two kinds of sums (rounds_weights)
   const size_t partials = partials_bytes(ctx, segs, p.head_dim, exact);  // then the plan
   if (!direct) {
     const int32_t rc = tiled_workspace(ctx, stream, partials + plan_bytes(p.batch), &ws);
