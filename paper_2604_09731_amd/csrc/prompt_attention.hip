@@ -745,12 +745,9 @@ __global__ __launch_bounds__(kWaves* kWave, D == 64 && N == 2 ? 3 : 2) void prom
       next_stage();
     }
   };
-  // Stages that all rows of the wavefront see whole lie between (one loop of each kind: a second copy of the edges' takes registers
-  // that the loops do not have).
-  const int whole = mine < rows ? (first + 1) / S::kKeys : 0;
-  for (int pass = kWindow ? 0 : 1; pass < 2; ++pass) {
-    const int inside = pass == 1 ? whole : 0;
-    while (t < inside) {
+  // Stages that all rows of the wavefront see whole.
+  auto inside = [&](int until) {
+    while (t < until) {
 #pragma unroll
       for (int part = 0; part < 2; ++part) {
         x.softmax(pb, s, a.c, v, at, part);
@@ -766,8 +763,18 @@ __global__ __launch_bounds__(kWaves* kWave, D == 64 && N == 2 ? 3 : 2) void prom
       }
       next_stage();
     }
-    // where the windows begin; the diagonal and the prompt's end
-    edge(pass == 1 ? steps : min(steps, last >= span.window ? (last - span.window) / S::kKeys + 1 : 0));
+  };
+  const int whole = mine < rows ? (first + 1) / S::kKeys : 0;
+  if constexpr (kWindow) {
+    // Where the windows begin; between the edges; the diagonal and the prompt's end.  (One loop of each kind: a second copy of the
+    // edges' takes registers that the loops do not have.)
+    for (int pass = 0; pass < 2; ++pass) {
+      inside(pass == 1 ? whole : 0);
+      edge(pass == 1 ? steps : min(steps, last >= span.window ? (last - span.window) / S::kKeys + 1 : 0));
+    }
+  } else {
+    inside(whole);
+    edge(steps);  // the diagonal and the prompt's end
   }
   if (mine < rows) x.finish(a, base, g, mine, rows, lane);
 }
