@@ -51,7 +51,7 @@ struct PromptArgs {
   const int32_t* cu;
   int64_t q_stride, k_stride, v_stride, out_stride;
   int32_t batch, total_tokens, Hq, Hkv, G;
-  int32_t window, sinks;  // (at most total_tokens each)
+  int32_t window, sinks;  // 0 in calls without a window; less than total_tokens in all
   uint32_t num_cus;
   float scale, c;  // c: in powers of two
 };
@@ -869,8 +869,10 @@ int32_t prompt(smart_ctx* ctx, void* stream, const prompt_params& p, int32_t win
   a.Hq = p.num_q_heads;
   a.Hkv = p.num_kv_heads;
   a.G = p.num_q_heads / p.num_kv_heads;
-  a.window = window < p.total_tokens ? window : p.total_tokens;
-  a.sinks = sinks < p.total_tokens ? sinks : p.total_tokens;
+  // (the last token of the longest prompt there can be sees the first `sinks` and the last `window`: with all of them nothing is hidden)
+  const bool hides = window > 0 && (int64_t)window + sinks < p.total_tokens;
+  a.window = hides ? window : 0;
+  a.sinks = hides ? sinks : 0;
   a.num_cus = ctx->num_cus > 0 ? ctx->num_cus : 256;
   a.scale = p.softmax_scale;
   a.c = p.softmax_scale * kLog2e;
@@ -881,9 +883,7 @@ int32_t prompt(smart_ctx* ctx, void* stream, const prompt_params& p, int32_t win
   SMART_HIP_CHECK(hipGetDevice(&prev));
   if (prev != ctx->device) SMART_HIP_CHECK(hipSetDevice(ctx->device));
   hipStream_t s = (hipStream_t)stream;
-  // (a window that no prompt can fill hides nothing)
-  rc = window > 0 && window < p.total_tokens ? launch_any<true>(a, f32, p.head_dim, rows, threads, s)
-                                             : launch_any<false>(a, f32, p.head_dim, rows, threads, s);
+  rc = hides ? launch_any<true>(a, f32, p.head_dim, rows, threads, s) : launch_any<false>(a, f32, p.head_dim, rows, threads, s);
   if (prev != ctx->device) (void)hipSetDevice(prev);
   return rc;
 }
