@@ -603,6 +603,10 @@ struct RowsBf16 {
       for (int e = 0; e < 8; ++e) e2[r][e] = fmaf(raw[e], c, -now);
     }
   }
+  // A weight enters the output product as one bf16.  Three parts would hold its 24 bits, and make four products of the two that a
+  // (row, key) takes, where the matrix cores are what bounds the call.  It is off by 2^-8 of itself at most; the sum that divides is
+  // that of the rounded weights, so a row is off by 2 2^-8 of its weighted mean |V| at most, about what rounding the result may cost.
+  // (Against 64 bits on normal values: root mean square 0.0020 of the output's, 0.0016 of them from rounding the result.)
   __device__ void weights(bf16x8 (&pb)[N], const floatx8 (&e2)[N]) {
 #pragma unroll
     for (int r = 0; r < N; ++r) {

@@ -47,13 +47,15 @@
 // With a window (tree_verify_attention_window) the same kernels run over the keys that some node sees, numbered without the gap behind
 // the first tokens (Span): a step's keys are eight tokens by eight wherever they lie, and the tiles at the ends of the gap are masked row
 // by row.  Every kernel is compiled for both, so that calls without a window keep their code.  bf16: 64 sequences, 64 / 8 heads of
-// 128, window 4096, one token each 202 us (1.08 GB, 5.3 TB/s); 32 sequences of 100 .. 8192 tokens, 4 .. 64 nodes, 32 / 8 heads, window 1024
-// 87 (prefix kernel 62, finishing 23: vector work, half of the prefix kernel's issue); one of 5000, 7 nodes, window 512, 19 (11 and 6,
-// chains of loads); fp8 in plain pages, 12 of 1500 .. 8192, 10 .. 24 nodes, 28 / 4 heads, window 2000, 40 (29 and 11).  Tried and
-// dropped: the tree as a last step of the prefix kernel (its registers make the streaming loop spill: the 64 sequences 287 us); a
-// finishing kernel with the tree staged in LDS (the wide trees 37 us instead of 25), or on the matrix cores with 32 rows a wavefront
-// (18, but 17 and 10 instead of 11 and 6 where the trees are small); pages addressed from 32-bit strides (a sixteenth of the prefix
-// kernel's vector instructions: 60 -> 58.5).
+// 128, window 4096, one token each 203 us (1.08 GB, 5.3 TB/s); 32 sequences of 100 .. 8192 tokens, 4 .. 64 nodes, 32 / 8 heads, window 1024
+// 91 (prefix kernel 69, finishing 22: vector work, half of the prefix kernel's issue); one of 5000, 7 nodes, window 512, 19 (11 and 6,
+// chains of loads); fp8 in plain pages, 12 of 1500 .. 8192, 10 .. 24 nodes, 28 / 4 heads, window 2000, 43.5 (34 and 11).  With weights
+// rounded to one bf16 the four take 202, 87, 19 and 40.  Tried and dropped, with weights so rounded: the tree as a last step of the prefix
+// kernel (its registers make the streaming loop spill: the 64 sequences 287 us); a finishing kernel with the tree staged in LDS (the wide
+// trees 37 us instead of 25), or on the matrix cores with 32 rows a wavefront (18, but 17 and 10 instead of 11 and 6 where the trees are
+// small); pages addressed from 32-bit strides (a sixteenth of the prefix kernel's vector instructions: 60 -> 58.5).
+// The 4-bit cache is staged too: 32 sequences of 1024 keys, 4 .. 64 nodes, 80 us where streaming without a window takes 67, 16 single
+// tokens of 4096 keys 37.5 and 28.5.
 //
 // The paper (Sec. 1) has the target model verify the tree in one forward pass; this is the attention sub-step.
 #include <math.h>
@@ -144,7 +146,8 @@ template <> struct StepCost<float> { static constexpr int one = 4, two = 7, four
 
 // A prefix seen through a window: what some node sees of it, the first `sinks` tokens and those that the root's window holds, as
 // keys without the gap between them.  Key v is token v, or v + shift from `gap` on.  Gap and shift are multiples of 8: groups of eight
-// keys are groups of eight tokens, in one page.  No other page is read (the page of the first key holds a token that is seen).
+// keys are groups of eight tokens, in one page.  No other page is read: that of the first key behind the gap holds the first token that
+// the root's window does (behind a partly filled last page with a window of 1, where it would).
 template <bool kWindow>
 struct Span {
   int shift = 0, gap = 0;
@@ -1782,8 +1785,9 @@ __global__ __launch_bounds__(kThreads, 2) void tva_tiled_kernel(TiledArgs a) {
 // kParts = 0: a wavefront per eight rows goes through both.
 constexpr int finish_waves(int parts) { return parts > 0 ? 1 + parts : 4; }
 // With a window a wavefront that goes through both chains keeps less in flight (the next tree keys, what its segment's place follows
-// from), which leaves four a SIMD instead of three: 32 sequences of 4 .. 64 nodes 25 -> 23 us (the call 83.5 -> 80), 96 of 1 .. 20, window
-// 500, the call 85 -> 81.5; 12 of 10 .. 24, fp8, 11.7 -> 12.0.  (Five, or four with all of it in flight, spill: 43 us for the 25.)
+// from), which leaves four a SIMD instead of three: 32 sequences of 4 .. 64 nodes 25 -> 22 us (the call, many times over, 86 .. 92 -> 83 ..
+// 89), 96 of 1 .. 20, window 500, the call 88 .. 92 -> 87 .. 92; 12 of 10 .. 24, fp8, 42.5 .. 44.5 -> 43 .. 45.  (Five, or four with all of
+// it in flight, spill: 43 us for the 25.)
 template <typename T, int D>
 constexpr bool lean_finish(int parts, bool window) { return parts == 0 && window && D == 128 && sizeof(T) == 2; }
 template <typename T, int D, int kParts, bool kExact, bool kWindow>
